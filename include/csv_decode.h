@@ -20,6 +20,7 @@
 #ifndef CSV_DECODE_H
 #define CSV_DECODE_H
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -305,6 +306,95 @@ typedef struct {
 } csv_kmax_ctl;
 int csv_kmax_init(csv_kmax_ctl* c, int K0, int K_min, int K_cap, double alpha, double rho_target, int literal);
 int csv_kmax_update(csv_kmax_ctl* c, int n_fallback, int n_sequences);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Operators around the head: 4-bit microscaled rows and the product with a 4-bit head, log-probabilities of given
+ * tokens, the clipped policy loss.  All of them only enqueue work on `stream`, allocate nothing and never synchronise
+ * (csv_mx4_head_create and csv_mx4_head_free excepted), so they may be captured into a graph; scratch is the caller's
+ * and holds nothing between calls: calls that may overlap (other streams, other graphs) need scratch of their own.
+ * Zero rows are a valid request.  A pointer that a call does not need may be NULL.  The current device has to be the
+ * one the pointers and the stream belong to.
+ */
+#define CSV_F32  0   /* element types: float32 */
+#define CSV_BF16 1   /*                bfloat16 bit patterns */
+
+/*
+ * 4-bit microscaled rows.  A row of d elements (d % 8 == 0) is padded with zeros to dp = d rounded up to a multiple of
+ * 128 and cut into blocks of 32.  A block holds a scale 2^e, e = floor(log2 max|x|) - 2 clamped to -127..127 (-127 for
+ * a block of zeros), as the byte e + 127, and 32 elements x / 2^e rounded to the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6
+ * (ties to the even index, magnitudes above 6 to 6), as four bits: sign, then the index in that list.  The even element
+ * of a pair is the low half of its byte.  A block with a NaN or an infinity has the scale byte 255 and stands for NaNs.
+ * d_codes uint8[rows * dp/2] (16-byte aligned), d_scales uint8[rows * dp/32] (4-byte aligned), both row-major.
+ * csv_mx4_quantize: d_x [rows, d] of x_type with ld elements from one row to the next (ld >= d, ld % 8 == 0), 16-byte aligned.
+ * csv_mx4_dequantize writes the values that the rows stand for (exact in both types; beyond the type's range: infinite).
+ */
+int csv_mx4_quantize(const void* d_x, int x_type, int64_t ld, int rows, int d, uint8_t* d_codes, uint8_t* d_scales, void* stream);
+int csv_mx4_dequantize(const uint8_t* d_codes, const uint8_t* d_scales, int rows, int d, void* d_x, int x_type, int64_t ld, void* stream);
+
+/*
+ * A head of 4-bit microscaled rows: V rows of d elements in the format above (csv_mx4_quantize of W, or a checkpoint), laid
+ * out once for the matrix cores (what the padding of a row holds does not matter).  d_b DEVICE float32[V] or NULL.  The head keeps copies of its own (about V*d*0.53 bytes): the
+ * caller may free codes, scales and bias afterwards.  csv_mx4_head_create synchronises the stream before returning; on
+ * error *out is NULL.
+ */
+typedef struct csv_mx4_head csv_mx4_head;
+int csv_mx4_head_create(const uint8_t* d_codes, const uint8_t* d_scales, const float* d_b, int V, int d, void* stream,
+                        csv_mx4_head** out);
+int csv_mx4_head_dims(const csv_mx4_head* head, int* V, int* d);
+void csv_mx4_head_free(csv_mx4_head* head);
+
+/*
+ * Logits of a 4-bit head: d_logits[b*V + i] = <W_i, h_b> + b_i for B hidden states d_h bf16[B*d] (16-byte aligned), products
+ * exact, sums in float32, rounded once more where out_type is CSV_BF16.  act = CSV_ACT_BF16 takes h as it is (decode steps),
+ * CSV_ACT_MX4 rounds it to the 4-bit format first (many tokens: four times the matrix rate).  1 <= B <= CSV_MX4_MAX_BATCH, or 0.
+ * Scratch: csv_mx4_logits_scratch bytes, 16-byte aligned (none for CSV_ACT_BF16).
+ */
+#define CSV_ACT_BF16 0
+#define CSV_ACT_MX4  1
+#define CSV_MX4_MAX_BATCH 65536
+int csv_mx4_logits_scratch(const csv_mx4_head* head, int B, int act, size_t* bytes);
+int csv_mx4_logits(const csv_mx4_head* head, const uint16_t* d_h, int B, int act, void* d_logits, int out_type,
+                   void* d_scratch, size_t scratch_bytes, void* stream);
+
+/*
+ * Log-probabilities of given tokens.  x = row i of d_logits ([N, V] of `type`, ld >= V elements from row to row, any element
+ * alignment), c = inv_temperature > 0, t = d_tokens[i]:
+ *   m = max_j x_j,  s = sum_j exp(c (x_j - m)),   d_logp[i] = c (x_t - m) - ln s,   d_stats[2i] = m, d_stats[2i+1] = s.
+ * A token outside 0..V-1 leaves its row out: d_logp 0, d_stats (0, 0), and a gradient row of zeros.  Logits of minus infinity are masked tokens
+ * (probability 0); a row of nothing else has no distribution: d_logp minus infinity, s = 0, a gradient row of zeros.  A row
+ * with a NaN or a plus infinity gives NaN.
+ * csv_token_logprobs_backward: d_grad[i, j] = c g_i ([j = t] - exp(c (x_j - m)) / s) for g = d_grad_logp, in the type of the
+ * logits, from the d_stats of the forward call; d_grad may be d_logits (then ld_grad = ld).  A row with g_i = 0 is zeros and
+ * is not read.  Scratch: csv_loss_scratch bytes, 16-byte aligned, for the forward call.
+ */
+int csv_loss_scratch(int N, int V, size_t* bytes);
+int csv_token_logprobs(const void* d_logits, int type, int64_t ld, int N, int V, const int32_t* d_tokens, float inv_temperature,
+                       float* d_logp, float* d_stats, void* d_scratch, size_t scratch_bytes, void* stream);
+int csv_token_logprobs_backward(const void* d_logits, int type, int64_t ld, int N, int V, const int32_t* d_tokens,
+                                const float* d_stats, const float* d_grad_logp, float inv_temperature, void* d_grad,
+                                int64_t ld_grad, void* stream);
+
+/*
+ * Clipped policy loss with a KL term over N tokens, and its gradient by the logits, in one call.  With logp_i as above,
+ * r_i = exp(logp_i - d_old_logp[i]), A = d_advantages, w = d_weights (mask and normaliser in one: 1/n for a token that counts,
+ * 0 for one that does not), k_i = d_ref_logp[i] - logp_i:
+ *   *d_loss = sum_i w_i ( -min(r_i A_i, clip(r_i, 1 - clip_low, 1 + clip_high) A_i) + beta (exp(k_i) - k_i - 1) ),
+ *   d_grad[i, j] = g_i c ([j = t_i] - p_ij),   g_i = w_i ( -A_i r_i [A_i >= 0 ? r_i <= 1 + clip_high : r_i >= 1 - clip_low] + beta (1 - exp(k_i)) ).
+ * d_logp (or NULL) returns logp.  d_grad (or NULL: the loss alone) has the type of the logits and may be d_logits (then ld_grad =
+ * ld).  A row of weight 0, or of a token outside 0..V-1, is left out: nothing of it is read, d_logp 0, a gradient row of zeros.
+ * A row of minus infinities has logp minus infinity and a gradient row of zeros.  d_ref_logp is not read where beta is 0.
+ * The sum over rows is in float64 and in one order: equal calls (with rows at equal alignments) give equal bits.
+ */
+typedef struct {
+    float clip_low;        /* 0..1 */
+    float clip_high;       /* >= 0 (plus infinity: no upper clip) */
+    float beta;            /* >= 0, finite */
+    float inv_temperature; /* > 0, finite */
+} csv_policy_params;
+int csv_policy_loss(const void* d_logits, int type, int64_t ld, int N, int V, const int32_t* d_tokens,
+                    const float* d_old_logp, const float* d_ref_logp, const float* d_advantages, const float* d_weights,
+                    const csv_policy_params* params, float* d_loss, float* d_logp, void* d_grad, int64_t ld_grad,
+                    void* d_scratch, size_t scratch_bytes, void* stream);
 
 const char* csv_last_error(void);
 

@@ -19,6 +19,9 @@ FLAG_TOPK_CERT, FLAG_SOFTMAX_CERT, FLAG_FALLBACK, FLAG_INVALID_INPUT, FLAG_SOFTM
 SCHEDULE_ROUNDS, SCHEDULE_ALG1 = 0, 1
 COMBINE_ALL, COMBINE_ANY = 0, 1
 MAX_K, MAX_CLUSTERS, MAX_BATCH = 1024, 8192, 256
+F32, BF16 = 0, 1
+ACT_BF16, ACT_MX4 = 0, 1
+MX4_MAX_BATCH = 65536
 
 EXPORTS = [
     "csv_build_index", "csv_index_from_arrays", "csv_index_export", "csv_index_dims", "csv_index_free",
@@ -27,6 +30,9 @@ EXPORTS = [
     "csv_workspace_set_spin_limit", "csv_index_use_bf16_centroids",
     "csv_workspace_set_tail_split", "csv_bounds_static", "csv_index_set_bias_table", "csv_index_get_bias_table",
     "csv_index_set_angular", "csv_index_get_angular",
+    "csv_mx4_quantize", "csv_mx4_dequantize", "csv_mx4_head_create", "csv_mx4_head_dims", "csv_mx4_head_free",
+    "csv_mx4_logits_scratch", "csv_mx4_logits", "csv_loss_scratch", "csv_token_logprobs", "csv_token_logprobs_backward",
+    "csv_policy_loss",
 ]
 PROFILE_STAGES = ["bounds", "round0", "tail"]
 
@@ -45,6 +51,10 @@ class StepParams(C.Structure):
 class KmaxCtl(C.Structure):
     _fields_ = [("K_max", C.c_double), ("alpha", C.c_double), ("rho_target", C.c_double), ("K_min", C.c_int),
                 ("K_cap", C.c_int), ("literal", C.c_int)]
+
+
+class PolicyParams(C.Structure):
+    _fields_ = [("clip_low", C.c_float), ("clip_high", C.c_float), ("beta", C.c_float), ("inv_temperature", C.c_float)]
 
 
 class StepOut(C.Structure):
@@ -85,6 +95,19 @@ def _load() -> C.CDLL:
     lib.csv_workspace_set_spin_limit.argtypes = [vp, ci]
     lib.csv_index_use_bf16_centroids.argtypes = [vp, vp]
     lib.csv_workspace_set_tail_split.argtypes = [vp, ci]
+    i64, sz, cf = C.c_int64, C.c_size_t, C.c_float
+    lib.csv_mx4_quantize.argtypes = [vp, ci, i64, ci, ci, vp, vp, vp]
+    lib.csv_mx4_dequantize.argtypes = [vp, vp, ci, ci, vp, ci, i64, vp]
+    lib.csv_mx4_head_create.argtypes = [vp, vp, vp, ci, ci, vp, C.POINTER(vp)]
+    lib.csv_mx4_head_dims.argtypes = [vp, C.POINTER(ci), C.POINTER(ci)]
+    lib.csv_mx4_head_free.argtypes = [vp]
+    lib.csv_mx4_head_free.restype = None
+    lib.csv_mx4_logits_scratch.argtypes = [vp, ci, ci, C.POINTER(sz)]
+    lib.csv_mx4_logits.argtypes = [vp, vp, ci, ci, vp, ci, vp, sz, vp]
+    lib.csv_loss_scratch.argtypes = [ci, ci, C.POINTER(sz)]
+    lib.csv_token_logprobs.argtypes = [vp, ci, i64, ci, ci, vp, cf, vp, vp, vp, sz, vp]
+    lib.csv_token_logprobs_backward.argtypes = [vp, ci, i64, ci, ci, vp, vp, vp, cf, vp, i64, vp]
+    lib.csv_policy_loss.argtypes = [vp, ci, i64, ci, ci, vp, vp, vp, vp, vp, C.POINTER(PolicyParams), vp, vp, vp, i64, vp, sz, vp]
     return lib
 
 
@@ -362,6 +385,217 @@ def csv_full_logits(ws: CsvWorkspace, index: CsvIndex, h: torch.Tensor, out: tor
         out = torch.empty((B, index.V), dtype=torch.float32, device=h.device)
     _check(lib.csv_full_logits(ws._h, index._h, h.data_ptr(), B, out.data_ptr(), _stream(stream)))
     return out
+
+
+_TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.int16: BF16}     # int16: bf16 patterns
+
+
+def _rows(t: torch.Tensor, what: str) -> int:
+    """The element type of a [rows, columns] tensor on the current device whose rows are contiguous."""
+    ty = _TYPES.get(t.dtype)
+    if ty is None or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what} must be 2-D float32 or bfloat16 with contiguous rows")
+    _here(t, what)
+    return ty
+
+
+def _ld(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _here(t: torch.Tensor, what: str) -> None:
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{what} must be on the current CUDA device")
+
+
+def _dense(t: torch.Tensor, what: str, dtype, *shape) -> int:
+    """Pointer of a contiguous tensor of this type and shape on the current device."""
+    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {shape}")
+    _here(t, what)
+    return t.data_ptr()
+
+
+class _On:
+    """What a call allocates belongs to the stream that the call runs on."""
+
+    def __init__(self, stream):
+        self._guard = None if stream is None else torch.cuda.stream(stream)
+
+    def __enter__(self):
+        if self._guard is not None:
+            self._guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self._guard is not None:
+            self._guard.__exit__(*exc)
+
+
+def _scratch(need: int, scratch, device) -> tuple:
+    """(tensor that keeps the memory alive, pointer, bytes); the caller's scratch where it is given."""
+    if scratch is not None:
+        _here(scratch, "scratch")
+        if not scratch.is_contiguous():
+            raise ValueError("scratch must be contiguous")
+        return scratch, scratch.data_ptr(), scratch.numel() * scratch.element_size()
+    if need == 0:
+        return None, None, 0
+    t = torch.empty(need, dtype=torch.uint8, device=device)
+    return t, t.data_ptr(), need
+
+
+def mx4_padded(d: int) -> int:
+    """Elements of a 4-bit row with its padding: two per byte of codes, 32 per scale byte."""
+    return (d + 127) // 128 * 128
+
+
+def csv_mx4_quantize(x: torch.Tensor, codes: torch.Tensor | None = None, scales: torch.Tensor | None = None, stream=None):
+    """(codes uint8 [rows, dp/2], scales uint8 [rows, dp/32]) of the rows of x, bfloat16 or float32 [rows, d]."""
+    ty = _rows(x, "x")
+    rows, d = x.shape
+    dp = mx4_padded(d)
+    with _On(stream):
+        if codes is None:
+            codes = torch.empty((rows, dp // 2), dtype=torch.uint8, device=x.device)
+        if scales is None:
+            scales = torch.empty((rows, dp // 32), dtype=torch.uint8, device=x.device)
+        _check(lib.csv_mx4_quantize(x.data_ptr(), ty, _ld(x), rows, d, _dense(codes, "codes", torch.uint8, rows, dp // 2),
+                                    _dense(scales, "scales", torch.uint8, rows, dp // 32), _stream(stream)))
+    return codes, scales
+
+
+def csv_mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, d: int, out: torch.Tensor | None = None, dtype=torch.bfloat16, stream=None):
+    """The values [rows, d] that codes and scales stand for."""
+    rows, dp = codes.shape[0], mx4_padded(d)
+    with _On(stream):
+        if out is None:
+            out = torch.empty((rows, d), dtype=dtype, device=codes.device)
+        ty = _rows(out, "out")
+        if tuple(out.shape) != (rows, d):
+            raise ValueError(f"out must have the shape {(rows, d)}")
+        _check(lib.csv_mx4_dequantize(_dense(codes, "codes", torch.uint8, rows, dp // 2), _dense(scales, "scales", torch.uint8, rows, dp // 32),
+                                      rows, d, out.data_ptr(), ty, _ld(out), _stream(stream)))
+    return out
+
+
+class CsvMx4Head:
+    """Owner of a csv_mx4_head handle."""
+
+    def __init__(self, handle: int):
+        self._h = C.c_void_p(handle)
+        V, d = C.c_int(), C.c_int()
+        _check(lib.csv_mx4_head_dims(self._h, C.byref(V), C.byref(d)))
+        self.V, self.d = V.value, d.value
+
+    def free(self) -> None:
+        if self._h:
+            lib.csv_mx4_head_free(self._h)
+            self._h = C.c_void_p(0)
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+
+def csv_mx4_head(codes: torch.Tensor, scales: torch.Tensor, b, d: int, stream=None) -> CsvMx4Head:
+    """A head of 4-bit rows [V, d] (csv_mx4_quantize of W, or a checkpoint), laid out for csv_mx4_logits; b: float32 CUDA [V] or None."""
+    V, dp = codes.shape[0], mx4_padded(d)
+    out = C.c_void_p()
+    _check(lib.csv_mx4_head_create(_dense(codes, "codes", torch.uint8, V, dp // 2), _dense(scales, "scales", torch.uint8, V, dp // 32),
+                                   None if b is None else _dense(b, "b", torch.float32, V), V, d, _stream(stream), C.byref(out)))
+    return CsvMx4Head(out.value)
+
+
+def csv_mx4_logits(head: CsvMx4Head, h: torch.Tensor, out: torch.Tensor | None = None, act: int = ACT_BF16, dtype=torch.float32,
+                   scratch: torch.Tensor | None = None, stream=None):
+    """Logits [B, V] of hidden states h [B, d] (bf16 patterns) from a 4-bit head; act ACT_MX4 rounds h to 4 bits first."""
+    _dev2(h, "h")
+    _here(h, "h")
+    if h.dim() != 2 or h.shape[1] != head.d or h.dtype not in (torch.bfloat16, torch.int16):
+        raise ValueError(f"h must be [B, {head.d}] in bfloat16")
+    B = h.shape[0]
+    with _On(stream):
+        if out is None:
+            out = torch.empty((B, head.V), dtype=dtype, device=h.device)
+        ty = _TYPES.get(out.dtype)
+        if ty is None:
+            raise ValueError("out must be float32 or bfloat16")
+        need = C.c_size_t()
+        _check(lib.csv_mx4_logits_scratch(head._h, B, act, C.byref(need)))
+        keep, ptr, size = _scratch(need.value, scratch, h.device)
+        _check(lib.csv_mx4_logits(head._h, h.data_ptr(), B, act, _dense(out, "out", out.dtype, B, head.V), ty, ptr, size, _stream(stream)))
+    return out
+
+
+def csv_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, inv_temperature: float = 1.0, logp: torch.Tensor | None = None,
+                       stats: torch.Tensor | None = None, scratch: torch.Tensor | None = None, stream=None):
+    """(logp float32 [N], stats float32 [N, 2]) of tokens int32 [N] under logits [N, V], float32 or bfloat16."""
+    ty = _rows(logits, "logits")
+    N, V = logits.shape
+    with _On(stream):
+        if logp is None:
+            logp = torch.empty(N, dtype=torch.float32, device=logits.device)
+        if stats is None:
+            stats = torch.empty((N, 2), dtype=torch.float32, device=logits.device)
+        need = C.c_size_t()
+        _check(lib.csv_loss_scratch(N, V, C.byref(need)))
+        keep, ptr, size = _scratch(need.value, scratch, logits.device)
+        _check(lib.csv_token_logprobs(logits.data_ptr(), ty, _ld(logits), N, V, _dense(tokens, "tokens", torch.int32, N), inv_temperature,
+                                      _dense(logp, "logp", torch.float32, N), _dense(stats, "stats", torch.float32, N, 2), ptr, size,
+                                      _stream(stream)))
+    return logp, stats
+
+
+def _grad_of(logits: torch.Tensor, grad: torch.Tensor) -> tuple:
+    if _rows(grad, "grad") != _TYPES[logits.dtype] or grad.shape != logits.shape:
+        raise ValueError("grad must have the type and the shape of the logits")
+    return grad.data_ptr(), _ld(grad)
+
+
+def csv_token_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor, stats: torch.Tensor, grad_logp: torch.Tensor,
+                                inv_temperature: float = 1.0, grad: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """The gradient by the logits, [N, V] in their type, from the stats of csv_token_logprobs and the gradient by logp (float32 [N]).
+    grad may be the logits themselves."""
+    ty = _rows(logits, "logits")
+    N, V = logits.shape
+    with _On(stream):
+        if grad is None:
+            grad = torch.empty((N, V), dtype=logits.dtype, device=logits.device)
+        gp, gld = _grad_of(logits, grad)
+        _check(lib.csv_token_logprobs_backward(logits.data_ptr(), ty, _ld(logits), N, V, _dense(tokens, "tokens", torch.int32, N),
+                                               _dense(stats, "stats", torch.float32, N, 2), _dense(grad_logp, "grad_logp", torch.float32, N),
+                                               inv_temperature, gp, gld, _stream(stream)))
+    return grad
+
+
+def csv_policy_loss(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.Tensor, ref_logp: torch.Tensor | None, advantages: torch.Tensor,
+                    weights: torch.Tensor, clip_low: float = 0.2, clip_high: float = 0.2, beta: float = 0.0, inv_temperature: float = 1.0,
+                    loss: torch.Tensor | None = None, logp: torch.Tensor | None = None, grad: torch.Tensor | None = None, want_grad: bool = True,
+                    scratch: torch.Tensor | None = None, stream=None):
+    """(loss float32 scalar tensor, logp float32 [N], grad [N, V] in the type of the logits, or None without want_grad and grad) of the
+    clipped policy loss; weights are mask and normaliser in one.  grad may be the logits themselves."""
+    ty = _rows(logits, "logits")
+    N, V = logits.shape
+    f32 = torch.float32
+    with _On(stream):
+        if loss is None:
+            loss = torch.empty((), dtype=f32, device=logits.device)
+        if logp is None:
+            logp = torch.empty(N, dtype=f32, device=logits.device)
+        if grad is None and want_grad:
+            grad = torch.empty((N, V), dtype=logits.dtype, device=logits.device)
+        gp, gld = (None, 0) if grad is None else _grad_of(logits, grad)
+        params = PolicyParams(clip_low, clip_high, beta, inv_temperature)
+        need = C.c_size_t()
+        _check(lib.csv_loss_scratch(N, V, C.byref(need)))
+        keep, ptr, size = _scratch(need.value, scratch, logits.device)
+        _check(lib.csv_policy_loss(logits.data_ptr(), ty, _ld(logits), N, V, _dense(tokens, "tokens", torch.int32, N),
+                                   _dense(old_logp, "old_logp", f32, N), None if ref_logp is None else _dense(ref_logp, "ref_logp", f32, N),
+                                   _dense(advantages, "advantages", f32, N), _dense(weights, "weights", f32, N), C.byref(params),
+                                   _dense(loss, "loss", f32), _dense(logp, "logp", f32, N), gp, gld, ptr, size, _stream(stream)))
+    return loss, logp, grad
 
 
 def bits_to_device(bits) -> torch.Tensor:

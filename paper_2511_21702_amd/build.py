@@ -11,7 +11,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcsvdecode.so")
 OBJ_DIR = os.path.join(HERE, "_build")
-SOURCES = ["csv_step.hip", "csv_index.hip"]
+SOURCES = ["csv_step.hip", "csv_index.hip", "csv_mx4.hip", "csv_loss.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

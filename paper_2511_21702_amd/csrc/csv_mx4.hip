@@ -1,0 +1,340 @@
+// 4-bit microscaled rows and the product with a head of such rows.
+//
+//   quantize_kernel     blocks of 32 elements -> one scale byte and 32 four-bit codes, row-major or in matrix-core tiles
+//   dequantize_kernel   the values that row-major codes stand for
+//   lay_out_kernel      row-major codes of a head -> tiles
+//   logits_kernel       out[b, i] = <W_i, h_b> + b_i on the matrix cores
+//
+// A tile is 16 rows x 128 elements: lane l of a wave holds the 32 elements of block l / 16 of row l % 16 (16 bytes) and that
+// block's scale, which is how v_mfma_scale_f32_16x16x128_f8f6f4 takes an operand.  Codes of a tile are 1 KB in lane order; the
+// scales of four tiles that follow each other along the row are one dword per lane, byte c for tile c.
+#include "csv_common.h"
+
+#include <stdlib.h>
+
+#define BLK 32        // elements of a block
+#define CHUNK 128     // elements of a row in a tile; rows are padded to a multiple of it
+#define HEAD_ROWS 256 // rows of a head are padded to a multiple of it (with codes 0), so that no product kernel tests a row before it stores
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v2f __attribute__((ext_vector_type(2)));
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+
+struct csv_mx4_head {
+    int V, d, device;
+    int chunks;         // tiles along a row
+    uint8_t* codes;     // [rows16 / 16][chunks][1024]
+    uint32_t* scales;   // [rows16 / 16][(chunks + 3) / 4][64]
+    float* bias;        // [V] or NULL
+};
+
+static inline int chunks_of(int d) { return (d + CHUNK - 1) / CHUNK; }
+
+// ------------------------------------------------------------------------------------------------ rounding
+// Eight elements of a lane; four lanes hold a block.  The scale is taken from the exponent field of the largest magnitude alone:
+// floor(log2) of a normal float32 is its field - 127, and every subnormal is below the smallest scale anyway.
+// x * 2^-e is exact (a result below float32's range rounds to 0 either way), so the one rounding is the conversion's, to nearest even.
+struct Elems8 {
+    float v[8];
+};
+__device__ __forceinline__ Elems8 load8(const uint16_t* p) {
+    const uint4 u = *(const uint4*)p;
+    return {{bf16_lo(u.x), bf16_hi(u.x), bf16_lo(u.y), bf16_hi(u.y), bf16_lo(u.z), bf16_hi(u.z), bf16_lo(u.w), bf16_hi(u.w)}};
+}
+__device__ __forceinline__ Elems8 load8(const float* p) {
+    const float4 a = ((const float4*)p)[0], b = ((const float4*)p)[1];
+    return {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+}
+__device__ __forceinline__ uint32_t round8(const Elems8& x, uint32_t& scale) {
+    uint32_t m = 0;
+    for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(x.v[j]) & 0x7fffffffu);
+    m = max(m, (uint32_t)dpp_move<0xB1, 0xf>((int)m, (int)m));   // quad_perm [1,0,3,2]
+    m = max(m, (uint32_t)dpp_move<0x4E, 0xf>((int)m, (int)m));   // quad_perm [2,3,0,1]
+    const uint32_t field = m >> 23;
+    scale = field == 255u ? 255u : field > 2u ? field - 2u : 0u;
+    const float inv = __uint_as_float((254u - (scale == 255u ? 0u : scale)) << 23);
+    uint32_t r = 0;
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x.v[0] * inv, x.v[1] * inv, 1.0f, 0);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x.v[2] * inv, x.v[3] * inv, 1.0f, 1);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x.v[4] * inv, x.v[5] * inv, 1.0f, 2);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x.v[6] * inv, x.v[7] * inv, 1.0f, 3);
+    return scale == 255u ? 0u : r;
+}
+
+// One wave: 512 elements of a row (blockIdx.x), rows blockIdx.y * 4 + wave and every 4 * gridDim.y rows further.  TILES: codes and scales go
+// to tiles; rows past `rows` (up to rows_out) are zeros.
+template <typename T, bool TILES>
+__global__ __launch_bounds__(256) void quantize_kernel(const T* __restrict__ x, int64_t ld, int rows, int rows_out, int d, int chunks,
+                                                        uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+    const int lane = threadIdx.x & 63, e0 = blockIdx.x * 512 + lane * 8, dp = chunks * CHUNK;
+    if (e0 >= dp) return;                                        // whole quads leave: dp is a multiple of 128
+    for (int row = blockIdx.y * 4 + (threadIdx.x >> 6); row < rows_out; row += 4 * gridDim.y) {
+        Elems8 v = {};
+        if (row < rows && e0 < d) v = load8(x + (int64_t)row * ld + e0);
+        uint32_t s;
+        const uint32_t c = round8(v, s);
+        if (TILES) {
+            const int tile = row >> 4, chunk = e0 >> 7, blk = (e0 >> 5) & 3, l = blk * 16 + (row & 15);
+            *(uint32_t*)(codes + ((int64_t)tile * chunks + chunk) * 1024 + l * 16 + ((e0 >> 1) & 15)) = c;
+            if ((lane & 3) == 0) scales[(((int64_t)tile * ((chunks + 3) >> 2) + (chunk >> 2)) * 64 + l) * 4 + (chunk & 3)] = (uint8_t)s;
+        } else {
+            *(uint32_t*)(codes + (int64_t)row * (dp >> 1) + (e0 >> 1)) = c;
+            if ((lane & 3) == 0) scales[(int64_t)row * (dp >> 5) + (e0 >> 5)] = (uint8_t)s;
+        }
+    }
+}
+
+__device__ __forceinline__ void store8(float* p, const float* v) {
+    ((float4*)p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    ((float4*)p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+// the values have two significant bits: the high half of the float32 pattern is the bfloat16
+__device__ __forceinline__ void store8(uint16_t* p, const float* v) {
+    uint32_t w[4];
+    for (int j = 0; j < 4; ++j) w[j] = (__float_as_uint(v[2 * j]) >> 16) | (__float_as_uint(v[2 * j + 1]) & 0xffff0000u);
+    *(uint4*)p = make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <typename T>
+__global__ __launch_bounds__(256) void dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int rows, int d, int chunks,
+                                                          T* __restrict__ x, int64_t ld) {
+    const int lane = threadIdx.x & 63, e0 = blockIdx.x * 512 + lane * 8, dp = chunks * CHUNK;
+    if (e0 >= d) return;
+    for (int row = blockIdx.y * 4 + (threadIdx.x >> 6); row < rows; row += 4 * gridDim.y) {
+        const uint32_t c = *(const uint32_t*)(codes + (int64_t)row * (dp >> 1) + (e0 >> 1));
+        const float s = __uint_as_float((uint32_t)scales[(int64_t)row * (dp >> 5) + (e0 >> 5)] << 23);   // exponent field 0: 2^-127; 255: NaN
+        const v2f a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 1),
+                  e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 2), f = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 3);
+        const float v[8] = {a[0], a[1], b[0], b[1], e[0], e[1], f[0], f[1]};
+        store8(x + (int64_t)row * ld + e0, v);
+    }
+}
+
+// One thread: 16 bytes of a tile, and where it is the first tile of four a dword of scales.  What the padding of a row holds is not taken over.
+__global__ __launch_bounds__(256) void lay_out_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int V, int d, int chunks, int64_t pieces,
+                                                       uint8_t* __restrict__ to, uint32_t* __restrict__ to_scales) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= pieces) return;
+    const int l = (int)(i & 63), g = l >> 4;
+    const int64_t t = i >> 6;
+    const int chunk = (int)(t % chunks);
+    const int64_t tile = t / chunks, row = tile * 16 + (l & 15);
+    uint4 c = make_uint4(0, 0, 0, 0);
+    const int left = d - chunk * CHUNK - g * BLK;      // elements of the row from this block on, a multiple of 8
+    if (row < V && left > 0) {
+        c = *(const uint4*)(codes + row * chunks * 64 + chunk * 64 + g * 16);
+        if (left <= 24) c.w = 0;
+        if (left <= 16) c.z = 0;
+        if (left <= 8) c.y = 0;
+    }
+    *(uint4*)(to + i * 16) = c;
+    if ((chunk & 3) == 0) {
+        uint32_t s = 0;
+        for (int k = 0; k < 4; ++k)
+            if (row < V && left > k * CHUNK) s |= (uint32_t)scales[(row * chunks + chunk + k) * 4 + g] << (8 * k);
+        to_scales[(tile * ((chunks + 3) >> 2) + (chunk >> 2)) * 64 + l] = s;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ product
+struct LogitsArgs {
+    const uint8_t* codes;
+    const uint32_t* scales;
+    const float* bias;
+    int V, d, chunks, B;
+    const uint16_t* h;          // bf16 [B, d]
+    const uint8_t* hc;          // or 4-bit tiles of it
+    const uint32_t* hs;
+    void* out;
+};
+
+__device__ __forceinline__ v8i widen(const uint4& u) { return v8i{(int)u.x, (int)u.y, (int)u.z, (int)u.w, 0, 0, 0, 0}; }
+__device__ __forceinline__ v8bf bf16_of_fp4(uint32_t c, float s) {
+    const v2bf a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1),
+               e = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2), f = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3);
+    return v8bf{a[0], a[1], b[0], b[1], e[0], e[1], f[0], f[1]};
+}
+__device__ __forceinline__ void store1(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store1(uint16_t* p, float v) { *p = __builtin_bit_cast(uint16_t, (__bf16)v); }
+
+// One wave: 16 rows x 16 hidden states.  The sum over k runs in the order of the storage, so both forms of the second operand put element
+// 32 (l / 16) + 8 s + j of a tile at lane l: a 4-bit tile goes to one matrix instruction as it is, against bf16 it is widened (exactly)
+// to four operands s = 0..3 of 16x16x32.
+template <bool MX4, typename T>
+__global__ __launch_bounds__(256) void logits_kernel(LogitsArgs a) {
+    const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
+    const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int quads = (a.chunks + 3) >> 2;
+    const uint8_t* wc = a.codes + tile * a.chunks * 1024 + lane * 16;
+    const uint32_t* ws = a.scales + tile * quads * 64 + lane;
+    const int b = blockIdx.y * 16 + col;
+    v4f acc = {0.f, 0.f, 0.f, 0.f};
+    for (int c = 0; c < a.chunks; ++c) {
+        const uint4 w = *(const uint4*)(wc + (int64_t)c * 1024);
+        const uint32_t s = ws[(c >> 2) * 64] >> (8 * (c & 3)) & 255u;
+        if (MX4) {
+            const int64_t ht = (int64_t)blockIdx.y * a.chunks + c;
+            const uint4 x = *(const uint4*)(a.hc + ht * 1024 + lane * 16);
+            const uint32_t xs = a.hs[((int64_t)blockIdx.y * quads + (c >> 2)) * 64 + lane] >> (8 * (c & 3)) & 255u;
+            acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widen(w), widen(x), acc, 4, 4, 0, s, 0, xs);
+        } else {
+            const float sf = __uint_as_float(s << 23);
+            const uint32_t q[4] = {w.x, w.y, w.z, w.w};
+            for (int k = 0; k < 4; ++k) {
+                const int e = c * CHUNK + g * BLK + k * 8;
+                uint4 x = make_uint4(0, 0, 0, 0);
+                if (b < a.B && e < a.d) x = *(const uint4*)(a.h + (int64_t)b * a.d + e);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of_fp4(q[k], sf), __builtin_bit_cast(v8bf, x), acc, 0, 0, 0);
+            }
+        }
+    }
+    if (b >= a.B) return;
+    T* out = (T*)a.out + (int64_t)b * a.V;
+    for (int r = 0; r < 4; ++r) {
+        const int64_t row = tile * 16 + g * 4 + r;
+        if (row < a.V) store1(out + row, acc[r] + (a.bias ? a.bias[row] : 0.f));
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ entry points
+static int check_rows(int rows, int d, int type, int64_t ld, const void* x, const uint8_t* codes, const uint8_t* scales) {
+    if (rows < 0 || d < 8 || (d & 7) != 0) { csv_set_error("need rows >= 0 and d a positive multiple of 8 (rows=%d, d=%d)", rows, d); return CSV_ESHAPE; }
+    if (type != CSV_F32 && type != CSV_BF16) { csv_set_error("bad element type %d", type); return CSV_EINVAL; }
+    if (ld < d || (ld & 7) != 0) { csv_set_error("row stride %lld is below d=%d or no multiple of 8", (long long)ld, d); return CSV_ESHAPE; }
+    if (rows == 0) return CSV_OK;
+    if (!x || !codes || !scales) { csv_set_error("null rows, codes or scales"); return CSV_EINVAL; }
+    if (((uintptr_t)x | (uintptr_t)codes) & 15) { csv_set_error("rows and codes have to be 16-byte aligned"); return CSV_EINVAL; }
+    if ((uintptr_t)scales & 3) { csv_set_error("scales have to be 4-byte aligned"); return CSV_EINVAL; }
+    return CSV_OK;
+}
+
+static dim3 rows_grid(int rows, int chunks) {
+    const int64_t y = ((int64_t)rows + 3) / 4;
+    return dim3((chunks + 3) / 4, (unsigned)(y < 32768 ? y : 32768));
+}
+
+extern "C" int csv_mx4_quantize(const void* d_x, int x_type, int64_t ld, int rows, int d, uint8_t* d_codes, uint8_t* d_scales, void* stream) {
+    const int rc = check_rows(rows, d, x_type, ld, d_x, d_codes, d_scales);
+    if (rc || rows == 0) return rc;
+    const int chunks = chunks_of(d);
+    const dim3 g = rows_grid(rows, chunks);
+    if (x_type == CSV_F32) quantize_kernel<float, false><<<g, 256, 0, (hipStream_t)stream>>>((const float*)d_x, ld, rows, rows, d, chunks, d_codes, d_scales);
+    else quantize_kernel<uint16_t, false><<<g, 256, 0, (hipStream_t)stream>>>((const uint16_t*)d_x, ld, rows, rows, d, chunks, d_codes, d_scales);
+    CSV_LAUNCH_CHECK("quantize_kernel");
+    return CSV_OK;
+}
+
+extern "C" int csv_mx4_dequantize(const uint8_t* d_codes, const uint8_t* d_scales, int rows, int d, void* d_x, int x_type, int64_t ld, void* stream) {
+    const int rc = check_rows(rows, d, x_type, ld, d_x, d_codes, d_scales);
+    if (rc || rows == 0) return rc;
+    const int chunks = chunks_of(d);
+    const dim3 g = rows_grid(rows, chunks);
+    if (x_type == CSV_F32) dequantize_kernel<float><<<g, 256, 0, (hipStream_t)stream>>>(d_codes, d_scales, rows, d, chunks, (float*)d_x, ld);
+    else dequantize_kernel<uint16_t><<<g, 256, 0, (hipStream_t)stream>>>(d_codes, d_scales, rows, d, chunks, (uint16_t*)d_x, ld);
+    CSV_LAUNCH_CHECK("dequantize_kernel");
+    return CSV_OK;
+}
+
+extern "C" int csv_mx4_head_create(const uint8_t* d_codes, const uint8_t* d_scales, const float* d_b, int V, int d, void* stream, csv_mx4_head** out) {
+    if (!out) { csv_set_error("null out"); return CSV_EINVAL; }
+    *out = nullptr;
+    if (!d_codes || !d_scales) { csv_set_error("null codes or scales"); return CSV_EINVAL; }
+    if (V < 1 || d < 8 || (d & 7) != 0) { csv_set_error("need V >= 1 and d a positive multiple of 8 (V=%d, d=%d)", V, d); return CSV_ESHAPE; }
+    if (V > 0x7fffffff - HEAD_ROWS) { csv_set_error("V=%d is too large", V); return CSV_ESHAPE; }
+    if ((uintptr_t)d_codes & 15) { csv_set_error("codes have to be 16-byte aligned"); return CSV_EINVAL; }
+    csv_mx4_head* x = (csv_mx4_head*)calloc(1, sizeof(csv_mx4_head));
+    if (!x) { csv_set_error("host allocation failed"); return CSV_ENOMEM; }
+    x->V = V;
+    x->d = d;
+    x->chunks = chunks_of(d);
+    const int64_t tiles = ((int64_t)V + HEAD_ROWS - 1) / HEAD_ROWS * (HEAD_ROWS / 16), pieces = tiles * x->chunks * 64;
+    const hipStream_t st = (hipStream_t)stream;
+    hipError_t e = hipGetDevice(&x->device);
+    if (e == hipSuccess) e = hipMalloc((void**)&x->codes, (size_t)pieces * 16);
+    if (e == hipSuccess) e = hipMalloc((void**)&x->scales, (size_t)tiles * ((x->chunks + 3) / 4) * 256);
+    if (e == hipSuccess && d_b) e = hipMalloc((void**)&x->bias, (size_t)V * 4);
+    if (e == hipSuccess && d_b) e = hipMemcpyAsync(x->bias, d_b, (size_t)V * 4, hipMemcpyDeviceToDevice, st);
+    if (e == hipSuccess) {
+        lay_out_kernel<<<(unsigned)((pieces + 255) / 256), 256, 0, st>>>(d_codes, d_scales, V, d, x->chunks, pieces, x->codes, x->scales);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess) e = hipStreamSynchronize(st);
+    if (e != hipSuccess) {
+        csv_set_error("head of %d x %d: %s", V, d, hipGetErrorString(e));
+        csv_mx4_head_free(x);
+        return e == hipErrorOutOfMemory ? CSV_ENOMEM : CSV_EHIP;
+    }
+    *out = x;
+    return CSV_OK;
+}
+
+extern "C" int csv_mx4_head_dims(const csv_mx4_head* x, int* V, int* d) {
+    if (!x) { csv_set_error("null head"); return CSV_EINVAL; }
+    if (V) *V = x->V;
+    if (d) *d = x->d;
+    return CSV_OK;
+}
+
+extern "C" void csv_mx4_head_free(csv_mx4_head* x) {
+    if (!x) return;
+    void* ptrs[] = {x->codes, x->scales, x->bias};
+    for (void* p : ptrs)
+        if (p) (void)hipFree(p);
+    free(x);
+}
+
+static int check_logits(const csv_mx4_head* x, int B, int act) {
+    if (!x) { csv_set_error("null head"); return CSV_EINVAL; }
+    if (B < 0 || B > CSV_MX4_MAX_BATCH) { csv_set_error("B=%d outside 0..%d", B, CSV_MX4_MAX_BATCH); return CSV_ESHAPE; }
+    if (act != CSV_ACT_BF16 && act != CSV_ACT_MX4) { csv_set_error("bad act=%d", act); return CSV_EINVAL; }
+    return CSV_OK;
+}
+// rows of the 4-bit copy of h: whole tiles
+static inline int64_t tiles16(int B) { return ((int64_t)B + 15) / 16; }
+
+extern "C" int csv_mx4_logits_scratch(const csv_mx4_head* x, int B, int act, size_t* bytes) {
+    const int rc = check_logits(x, B, act);
+    if (rc) return rc;
+    if (!bytes) { csv_set_error("null bytes"); return CSV_EINVAL; }
+    *bytes = act == CSV_ACT_BF16 ? 0 : (size_t)tiles16(B) * ((size_t)x->chunks * 1024 + (size_t)((x->chunks + 3) / 4) * 256);
+    return CSV_OK;
+}
+
+extern "C" int csv_mx4_logits(const csv_mx4_head* x, const uint16_t* d_h, int B, int act, void* d_logits, int out_type, void* d_scratch,
+                              size_t scratch_bytes, void* stream) {
+    size_t need = 0;
+    const int rc = csv_mx4_logits_scratch(x, B, act, &need);
+    if (rc) return rc;
+    if (out_type != CSV_F32 && out_type != CSV_BF16) { csv_set_error("bad element type %d", out_type); return CSV_EINVAL; }
+    if (B == 0) return CSV_OK;
+    if (!d_h || !d_logits) { csv_set_error("null h or d_logits"); return CSV_EINVAL; }
+    if ((uintptr_t)d_h & 15) { csv_set_error("h has to be 16-byte aligned"); return CSV_EINVAL; }
+    if ((uintptr_t)d_logits & (out_type == CSV_F32 ? 3 : 1)) { csv_set_error("d_logits is not aligned to its type"); return CSV_EINVAL; }
+    if (need && (!d_scratch || scratch_bytes < need)) { csv_set_error("scratch of %zu bytes, %zu are needed", d_scratch ? scratch_bytes : (size_t)0, need); return CSV_ESHAPE; }
+    if (need && ((uintptr_t)d_scratch & 15)) { csv_set_error("scratch has to be 16-byte aligned"); return CSV_EINVAL; }
+    int dev = -1;
+    CSV_HIP(hipGetDevice(&dev));
+    if (dev != x->device) { csv_set_error("the head lives on device %d, the current device is %d", x->device, dev); return CSV_EINVAL; }
+    const hipStream_t st = (hipStream_t)stream;
+    LogitsArgs a = {x->codes, x->scales, x->bias, x->V, x->d, x->chunks, B, d_h, nullptr, nullptr, d_logits};
+    const int64_t tt = tiles16(B);
+    if (act == CSV_ACT_MX4) {
+        uint8_t* hc = (uint8_t*)d_scratch;
+        uint8_t* hs = hc + (size_t)tt * x->chunks * 1024;
+        quantize_kernel<uint16_t, true><<<rows_grid((int)(tt * 16), x->chunks), 256, 0, st>>>(d_h, x->d, B, (int)(tt * 16), x->d, x->chunks, hc, hs);
+        CSV_LAUNCH_CHECK("quantize_kernel");
+        a.hc = hc;
+        a.hs = (const uint32_t*)hs;
+    }
+    const dim3 g((unsigned)((x->V + 63) / 64), (unsigned)tt);
+    if (act == CSV_ACT_MX4) {
+        if (out_type == CSV_F32) logits_kernel<true, float><<<g, 256, 0, st>>>(a);
+        else logits_kernel<true, uint16_t><<<g, 256, 0, st>>>(a);
+    } else {
+        if (out_type == CSV_F32) logits_kernel<false, float><<<g, 256, 0, st>>>(a);
+        else logits_kernel<false, uint16_t><<<g, 256, 0, st>>>(a);
+    }
+    CSV_LAUNCH_CHECK("logits_kernel");
+    return CSV_OK;
+}

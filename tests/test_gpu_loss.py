@@ -1,0 +1,303 @@
+"""Log-probabilities of given tokens, their gradient and the clipped policy loss against their definitions in float64."""
+import numpy as np
+import pytest
+
+from . import _operators as O
+from ._harness import log
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+F32, BF16 = torch.float32, torch.bfloat16
+HALF = {F32: 2.0 ** -24, BF16: 2.0 ** -8}             # half a step of the type, relative
+TINY = {F32: 2.0 ** -126, BF16: 2.0 ** -126}           # below this a step is absolute; the exponential returns 0 there
+
+
+def _csv():
+    import paper_2511_21702_amd as csv
+    return csv
+
+
+def _rows(N, V, dtype, seed, gap=0, shift=0):
+    """Logits [N, V] on the GPU as a view with `gap` elements between the rows that starts `shift` elements into its memory; tokens."""
+    gen = torch.Generator().manual_seed(seed)
+    x = torch.randn(N, V, generator=gen) * 3
+    t = torch.randint(0, V, (N,), generator=gen)
+    x[torch.arange(N), t] += 6 * torch.rand(N, generator=gen)
+    return _place(x, dtype, gap, shift), t.to(torch.int32).cuda()
+
+
+def _place(x, dtype, gap=0, shift=0, fill=float("nan")):
+    N, V = x.shape
+    mem = torch.full((shift + N * (V + gap) + 8,), fill, dtype=dtype, device="cuda")
+    v = mem[shift:shift + N * (V + gap)].view(N, V + gap)[:, :V]
+    v.copy_(x.to(dtype))
+    return v
+
+
+def _grad_close(got, p, s, t, g, c, rel, x, m, dtype):
+    """got against c g ([j = t] - p).  A probability carries the sum's error `rel` and, as in it, 4 U24 of its argument and one unit of the
+    exponential; coefficient, quotient, product and difference are rounded to float32 (4 U24 of what they make), the result to its type."""
+    want = O.grad_rows(p, s, t, g, c)
+    a = np.abs(c * (np.where(np.isfinite(x), x, m[:, None]) - m[:, None]))
+    cg = np.abs(c * g)[:, None]
+    tol = cg * p * (rel[:, None] + (4 * a + 8) * O.U24) + (np.abs(want) + cg * (p > 0.5)) * 4 * O.U24
+    tol = tol * (1 + HALF[dtype]) + HALF[dtype] * np.abs(want) + TINY[dtype] * (1 + cg)
+    with np.errstate(invalid="ignore"):
+        ok = (np.abs(got - want) <= tol) | (np.isnan(got) & np.isnan(want))
+    assert ok.all(), (np.argwhere(~ok)[:5], got[~ok][:5], want[~ok][:5])
+
+
+SHAPES = [(1, 1), (2, 2), (3, 5), (5, 33), (4, 255), (6, 1000), (3, 4097), (300, 515), (2, 8192), (3, 32003), (2, 70001), (2, 131073), (1, 300007)]
+
+
+@pytest.mark.parametrize("N,V", SHAPES)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("gap,shift,c", [(0, 0, 1.0), (3, 1, 0.7), (8, 0, 1.25)])
+def test_logprobs_and_their_gradient(N, V, dtype, gap, shift, c):
+    csv = _csv()
+    log(f"logprobs N={N} V={V} {dtype} gap={gap} shift={shift} c={c}")
+    c = float(np.float32(c))
+    x, t = _rows(N, V, dtype, N + V, gap, shift)
+    logp, stats = csv.csv_token_logprobs(x, t, c)
+    x64, t64 = x.cpu().double().numpy(), t.cpu().numpy()
+    m, s, want, p = O.rows_logp(x64, t64, c)
+    tol, rel = O.logp_tolerance(x64, m, p, c, want)
+    assert (np.abs(logp.cpu().double().numpy() - want) <= tol).all()
+    st = stats.cpu().double().numpy()
+    assert (st[:, 0] == m).all() and (np.abs(st[:, 1] - s) <= s * (rel + O.U24)).all()
+    g = torch.randn(N, generator=torch.Generator().manual_seed(N))
+    g[N // 2] = 0.0 if N > 2 else g[N // 2]
+    out = _place(torch.zeros(N, V), dtype, gap=5, shift=shift + (1 if gap else 0), fill=7.0)
+    got = csv.csv_token_logprobs_backward(x, t, stats, g.cuda(), c, grad=out)
+    _grad_close(got.cpu().double().numpy(), p, s, t64, g.double().numpy(), c, rel, x64, m, dtype)
+    assert bool(out._base[-8:].eq(7.0).all())
+    # into the logits' own memory, and twice: the same bits
+    again, st2 = csv.csv_token_logprobs(x, t, c)
+    assert torch.equal(again, logp) and torch.equal(st2, stats)
+    csv.csv_token_logprobs_backward(x, t, stats, g.cuda(), c, grad=x)
+    assert torch.equal(x, got)
+
+
+def _policy_inputs(logp, N, seed, skip=True):
+    rng = np.random.default_rng(seed)
+    # ratios away from the clip's borders by more than what a log-probability may be off
+    old = (logp - np.log(rng.choice([0.3, 0.7, 0.9, 1.0, 1.1, 1.25, 1.4, 2.0], N))).astype(np.float32)
+    ref = (logp + 0.4 * rng.normal(size=N)).astype(np.float32)
+    adv = rng.normal(size=N).astype(np.float32)
+    w = rng.uniform(0.1, 1.0, N).astype(np.float32) / N
+    if skip and N > 2:
+        w[rng.random(N) < 0.3] = 0.0
+        adv[0] = 0.0
+    return old, ref, adv, w
+
+
+def _policy_check(csv, x, t, c, lo, hi, beta, seed, dtype, in_place=False):
+    N, V = x.shape
+    x64, t64 = x.cpu().double().numpy(), t.cpu().numpy()
+    m, s, lp, p = O.rows_logp(x64, t64, c)
+    out = O.out_of_range(t64, V)
+    lp = np.where(out, 0.0, lp)
+    old, ref, adv, w = _policy_inputs(lp, N, seed)
+    d = [torch.from_numpy(a).cuda() for a in (old, ref, adv, w)]
+    before = x._base.clone().as_strided(x.shape, x.stride(), x.storage_offset())     # the same alignment: the same order of sums
+    loss, logp, grad = csv.csv_policy_loss(x, t, d[0], d[1] if beta > 0 else None, d[2], d[3], lo, hi, beta, c, grad=x if in_place else None)
+    terms, g = O.policy(lp, old.astype(float), ref.astype(float), adv.astype(float), w.astype(float), float(np.float32(lo)), float(np.float32(hi)), float(np.float32(beta)))
+    left = out | (w == 0)
+    terms, g, lp = np.where(left, 0.0, terms), np.where(left, 0.0, g), np.where(left, 0.0, lp)
+    tol, rel = O.logp_tolerance(x64, m, p, c, lp)
+    assert (np.abs(logp.cpu().double().numpy() - lp) <= np.where(left, 0.0, tol)).all()
+    # a log-probability that is off by rel moves a term and its derivative by at most rel times |w| (|A| r + beta exp(k)) and a little
+    r, k = np.exp(np.where(left, 0.0, lp - old)), np.exp(np.where(left, 0.0, ref - lp))
+    slope = np.abs(w) * (np.abs(adv) * r + beta * (k + 1.0))
+    assert abs(float(loss) - terms.sum()) <= (slope * rel).sum() * 1.01 + abs(terms.sum()) * O.U24 + 1e-30
+    relg = np.where(g != 0, slope * rel * 1.01 / np.maximum(np.abs(g), 1e-300), 0.0)
+    # the coefficient's own error moves the token's element as well
+    want = O.grad_rows(p, s, t64, g, c)
+    got = grad.cpu().double().numpy()
+    a = np.abs(c * (np.where(np.isfinite(x64), x64, m[:, None]) - m[:, None]))
+    cg = np.abs(c * g)[:, None]
+    gtol = cg * p * (rel[:, None] + (4 * a + 8) * O.U24) + (np.abs(want) + cg * (p > 0.5)) * 4 * O.U24 + np.abs(want) * relg[:, None]
+    gtol = gtol * (1 + HALF[dtype]) + HALF[dtype] * np.abs(want) + TINY[dtype] * (1 + cg)
+    ok = np.abs(got - want) <= gtol
+    assert ok.all(), (np.argwhere(~ok)[:5], got[~ok][:5], want[~ok][:5])
+    # the loss alone, and the same call again: the same bits
+    again = csv.csv_policy_loss(before, t, d[0], d[1] if beta > 0 else None, d[2], d[3], lo, hi, beta, c)
+    alone = csv.csv_policy_loss(before, t, d[0], d[1] if beta > 0 else None, d[2], d[3], lo, hi, beta, c, want_grad=False)
+    assert alone[2] is None and torch.equal(again[0], loss) and torch.equal(alone[0], loss)
+    assert torch.equal(again[1], logp) and torch.equal(alone[1], logp) and torch.equal(again[2], grad)
+
+
+@pytest.mark.parametrize("N,V", SHAPES)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("gap,shift,c,beta,hi,in_place", [(0, 0, 1.0, 0.0, 0.2, False), (5, 1, 0.7, 0.1, 0.28, False), (8, 0, 1.25, 0.04, float("inf"), True)])
+def test_policy_loss(N, V, dtype, gap, shift, c, beta, hi, in_place):
+    log(f"policy N={N} V={V} {dtype} gap={gap} shift={shift} c={c} beta={beta} hi={hi}")
+    x, t = _rows(N, V, dtype, N + V, gap, shift)
+    if N > 3:
+        t[1], t[3] = -1, V                               # rows that are left out
+    _policy_check(_csv(), x, t, float(np.float32(c)), 0.2, hi, beta, N + V, dtype, in_place)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V,N", [(1000, 8), (70001, 8), (1000, 700)])
+def test_masked_rows_and_values_that_are_not_finite(dtype, V, N):
+    csv = _csv()
+    x, t = _rows(N, V, dtype, 5)
+    inf, low = float("inf"), torch.finfo(dtype).min
+    x[0, V // 2:] = -inf
+    t[0] = 3
+    x[1] = -inf                                          # nothing is left
+    x[2, :] = low                                        # the lowest value everywhere: uniform
+    x[3, ::2] = low
+    t[3] = 1
+    x[4, 9] = inf
+    x[5, V - 1] = float("nan")
+    x[6, 11] = -inf
+    t[6] = 11                                            # the token itself is masked
+    t[7] = -1
+    logp, stats = csv.csv_token_logprobs(x, t)
+    x64, t64 = x.cpu().double().numpy(), t.cpu().numpy()
+    m, s, want, p = O.rows_logp(x64, t64, 1.0)
+    got = logp.cpu().double().numpy()
+    assert np.isneginf(got[1]) and np.isneginf(got[6]) and np.isnan(got[[4, 5]]).all() and got[7] == 0.0
+    fine = [i for i in range(N) if i not in (1, 4, 5, 6, 7)]
+    tol, rel = O.logp_tolerance(x64[fine], m[fine], p[fine], 1.0, want[fine])
+    assert (np.abs(got[fine] - want[fine]) <= tol).all()
+    g = torch.linspace(0.5, 1.5, N, device="cuda")
+    grad = csv.csv_token_logprobs_backward(x, t, stats, g).cpu().double().numpy()
+    assert (grad[[1, 7]] == 0).all() and np.isnan(grad[[4, 5]]).all()
+    assert (grad[0, V // 2:] == 0).all()
+    keep = fine + [6]
+    _grad_close(grad[keep], p[keep], s[keep], t64[keep], g.cpu().double().numpy()[keep], 1.0, np.append(rel, 600 * O.U24), x64[keep], m[keep], dtype)
+    # the policy loss: rows 4 and 5 by weight, 7 by token left out; row 1 has no gradient
+    w = torch.full((N,), 1.0 / N, device="cuda")
+    w[[4, 5]] = 0.0
+    adv = torch.ones(N, device="cuda")
+    old = torch.where(torch.isfinite(logp), logp, torch.zeros_like(logp))
+    loss, lp, grad = csv.csv_policy_loss(x, t, old, None, adv, w)
+    assert bool(torch.isfinite(loss)) and bool((grad[[1, 4, 5, 7]] == 0).all()) and bool(torch.isfinite(grad.float()).all())
+    assert np.isneginf(float(lp[1])) and bool((lp[[4, 5, 7]] == 0).all())
+    assert bool((grad[6] == 0).all())                    # ratio 0: no push either way
+    w[4] = 1.0 / N
+    loss, lp, grad = csv.csv_policy_loss(x, t, old, None, adv, w)
+    assert bool(torch.isnan(loss)) and bool(torch.isnan(grad[4].float()).all())
+
+
+def test_no_rows():
+    csv = _csv()
+    e = torch.empty(0, device="cuda")
+    loss, logp, grad = csv.csv_policy_loss(torch.empty(0, 50, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda"), e, None, e, e,
+                                           loss=torch.full((), 9.0, device="cuda"))
+    assert float(loss) == 0.0 and logp.numel() == 0 and tuple(grad.shape) == (0, 50)
+    logp, stats = csv.csv_token_logprobs(torch.empty(0, 50, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda"))
+    assert logp.numel() == 0
+    csv.csv_token_logprobs_backward(torch.empty(0, 50, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda"), stats, e)
+
+
+def test_all_rows_left_out():
+    csv = _csv()
+    x = torch.full((5, 4099), float("nan"), device="cuda")
+    z = torch.zeros(5, device="cuda")
+    loss, logp, grad = csv.csv_policy_loss(x, torch.zeros(5, dtype=torch.int32, device="cuda"), z, z, z, z, beta=0.1)
+    assert float(loss) == 0.0 and bool((logp == 0).all()) and bool((grad == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_rows_beyond_32_bits(dtype):
+    """More than 2^31 elements (and 2^32 bytes) of logits: the last rows are right, and the first."""
+    csv = _csv()
+    N, V = 17000, 130003
+    log(f"policy beyond 32 bits {dtype}")
+    x = torch.zeros(N, V, dtype=dtype, device="cuda")
+    t = torch.full((N,), 7, dtype=torch.int32, device="cuda")
+    rows = [0, N - 2, N - 1]
+    small, ts = _rows(3, V, dtype, 8)
+    x[rows], t[rows] = small, ts
+    w = torch.zeros(N, device="cuda")
+    w[rows] = torch.tensor([0.5, -0.25, 1.0], device="cuda")
+    one = torch.ones(N, device="cuda")
+    want = csv.csv_policy_loss(small, ts, -one[:3], None, one[:3], w[rows])
+    loss, logp, grad = csv.csv_policy_loss(x, t, -one, None, one, w, grad=x)
+    assert torch.equal(logp[rows], want[1]) and torch.equal(grad[rows], want[2])
+    assert abs(float(loss) - float(want[0])) <= 2 * O.U24 * abs(float(want[0]))
+    assert not bool(grad[1:N - 2].any())
+
+
+@pytest.mark.parametrize("N,V,dtype", [(3, 50021, F32), (700, 5003, BF16)])
+def test_captured_calls_and_a_stream_of_their_own(N, V, dtype):
+    csv = _csv()
+    c = 1.0
+    xs = [_rows(N, V, dtype, k)[0].contiguous() for k in range(3)]
+    t = _rows(N, V, dtype, 0)[1]
+    old = torch.full((N,), -5.0, device="cuda")
+    adv = torch.linspace(-1, 1, N, device="cuda")
+    w = torch.full((N,), 1.0 / N, device="cuda")
+
+    def both(x, stream=None):
+        loss, logp, grad = csv.csv_policy_loss(x, t, old, old, adv, w, beta=0.1, inv_temperature=c, stream=stream)
+        lp, stats = csv.csv_token_logprobs(x, t, c, stream=stream)
+        return [loss, logp, grad, lp, csv.csv_token_logprobs_backward(x, t, stats, adv, c, stream=stream)]
+
+    eager = [[v.clone() for v in both(x)] for x in xs]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = both(xs[1], stream=side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, eager[1]))
+    inp = [xs[0].clone() for _ in range(2)]
+    graphs, outs = [], []
+    for k in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(both(inp[k]))
+        graphs.append(g)
+    for i in range(4):
+        for k in range(2):
+            inp[k].copy_(xs[(i + k) % 3])
+            graphs[k].replay()
+        both(xs[2])
+        torch.cuda.synchronize()
+        for k in range(2):
+            assert all(torch.equal(a, b) for a, b in zip(outs[k], eager[(i + k) % 3]))
+
+
+def test_rollout_head_in_four_bits_then_policy_loss_on_the_exact_head():
+    """The operators in the order of a training step: the head in four bits samples and scores, the exact head's logits are trained against it."""
+    csv = _csv()
+    V, d, N = 2003, 264, 24
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    W = (torch.randn(V, d, generator=gen, device="cuda") * 0.15).to(BF16)
+    b = torch.randn(V, generator=gen, device="cuda") * 0.1
+    h = torch.randn(N, d, generator=gen, device="cuda").to(BF16)
+    idx = csv.csv_build_index(W, b, 8)
+    ws = csv.CsvWorkspace(idx, N, V)
+    full = csv.csv_full_logits(ws, idx, h)
+    codes, scales = csv.csv_mx4_quantize(W)
+    head = csv.csv_mx4_head(codes, scales, b, d)
+    roll = csv.csv_mx4_logits(head, h)
+    tokens = roll.argmax(1).to(torch.int32)
+    old, _ = csv.csv_token_logprobs(roll, tokens)
+    ref, _ = csv.csv_token_logprobs(csv.csv_mx4_logits(head, h, act=csv.ACT_MX4), tokens)
+    adv = torch.randn(N, generator=gen, device="cuda")
+    w = torch.full((N,), 1.0 / N, device="cuda")
+    loss, logp, grad = csv.csv_policy_loss(full, tokens, old, ref, adv, w, beta=0.05)
+    # the same from the operators' definitions, step by step from what the previous step gave
+    c64, s64 = O.mx4_quantize(O.bf16_values(W.cpu()))
+    assert np.array_equal(codes.cpu().numpy(), c64) and np.array_equal(scales.cpu().numpy(), s64)
+    W4 = O.mx4_values(c64, s64, d)
+    h64 = O.bf16_values(h.cpu())
+    want = h64 @ W4.T + b.cpu().double().numpy()
+    assert np.abs(roll.cpu().double().numpy() - want).max() <= 400 * O.U24 * (np.abs(h64) @ np.abs(W4).T).max()
+    x64, t64 = full.cpu().double().numpy(), tokens.cpu().numpy()
+    m, s, lp, p = O.rows_logp(x64, t64, 1.0)
+    terms, g = O.policy(lp, *[v.cpu().double().numpy() for v in (old, ref, adv, w)], float(np.float32(0.2)), float(np.float32(0.2)), float(np.float32(0.05)))
+    assert np.abs(logp.cpu().double().numpy() - lp).max() < 1e-5
+    assert abs(float(loss) - terms.sum()) < 1e-4
+    wantg = O.grad_rows(p, s, t64, g, 1.0)
+    r = np.exp(lp - old.cpu().double().numpy())
+    clear = (np.abs(r - 0.8) > 1e-3) & (np.abs(r - 1.2) > 1e-3)
+    assert clear.sum() > N // 2 and np.abs(grad.cpu().double().numpy() - wantg)[clear].max() < 1e-5
+    ws.free()
+    idx.free()
+    head.free()

@@ -1,0 +1,146 @@
+"""What the operators around the head refuse, and requests for nothing: no launch, so no GPU."""
+import ctypes as C
+import os
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+EINVAL, ESHAPE = -1, -4
+P = 4096                          # an address that no call may look at
+
+
+@pytest.fixture(scope="module")
+def csv():
+    if not os.path.exists(os.path.join(ROOT, "paper_2511_21702_amd", "libcsvdecode.so")):
+        import __graft_entry__
+        __graft_entry__.build()
+    import paper_2511_21702_amd
+    return paper_2511_21702_amd
+
+
+def test_rows_refused(csv):
+    q, dq = csv.lib.csv_mx4_quantize, csv.lib.csv_mx4_dequantize
+    for f in (lambda x, ty, ld, rows, d, c, s: q(x, ty, ld, rows, d, c, s, None), lambda x, ty, ld, rows, d, c, s: dq(c, s, rows, d, x, ty, ld, None)):
+        assert f(P, csv.BF16, 64, -1, 64, P, P) == ESHAPE
+        assert f(P, csv.BF16, 64, 4, 0, P, P) == ESHAPE
+        assert f(P, csv.BF16, 64, 4, 60, P, P) == ESHAPE           # d is no multiple of 8
+        assert f(P, csv.BF16, 56, 4, 64, P, P) == ESHAPE           # stride below d
+        assert f(P, csv.BF16, 68, 4, 64, P, P) == ESHAPE           # stride no multiple of 8
+        assert f(P, 2, 64, 4, 64, P, P) == EINVAL                  # unknown type
+        assert f(None, csv.BF16, 64, 4, 64, P, P) == EINVAL
+        assert f(P, csv.BF16, 64, 4, 64, None, P) == EINVAL
+        assert f(P, csv.BF16, 64, 4, 64, P, None) == EINVAL
+        assert f(P + 8, csv.BF16, 64, 4, 64, P, P) == EINVAL       # alignment
+        assert f(P, csv.BF16, 64, 4, 64, P + 4, P) == EINVAL
+        assert f(P, csv.BF16, 64, 4, 64, P, P + 2) == EINVAL
+        assert f(None, csv.F32, 64, 0, 64, None, None) == 0        # nothing to do
+
+
+def test_head_and_logits_refused(csv):
+    out = C.c_void_p(77)
+    make = csv.lib.csv_mx4_head_create
+    assert make(P, P, None, 16, 64, None, None) == EINVAL
+    for args in ((None, P, None, 16, 64), (P, None, None, 16, 64), (P + 4, P, None, 16, 64)):
+        out.value = 77
+        assert make(*args, None, C.byref(out)) == EINVAL and out.value is None
+    for V, d in ((0, 64), (16, 0), (16, 63), (2 ** 31 - 1, 64)):
+        out.value = 77
+        assert make(P, P, None, V, d, None, C.byref(out)) == ESHAPE and out.value is None
+    n = C.c_size_t()
+    assert csv.lib.csv_mx4_logits_scratch(None, 1, 0, C.byref(n)) == EINVAL
+    assert csv.lib.csv_mx4_logits(None, P, 1, 0, P, 0, None, 0, None) == EINVAL
+    assert b"null head" in csv.lib.csv_last_error()
+    assert csv.lib.csv_mx4_head_dims(None, None, None) == EINVAL
+    csv.lib.csv_mx4_head_free(None)
+
+
+def test_loss_refused(csv):
+    n = C.c_size_t()
+    assert csv.lib.csv_loss_scratch(-1, 5, C.byref(n)) == ESHAPE
+    assert csv.lib.csv_loss_scratch(1, 0, C.byref(n)) == ESHAPE
+    assert csv.lib.csv_loss_scratch(1, 5, None) == EINVAL
+    assert csv.lib.csv_loss_scratch(3, 70000, C.byref(n)) == 0 and n.value >= 24
+    big = 1 << 40
+
+    def fwd(x=P, ty=0, ld=100, N=3, V=100, t=P, c=1.0, logp=P, stats=P, scr=P, size=big):
+        return csv.lib.csv_token_logprobs(x, ty, ld, N, V, t, c, logp, stats, scr, size, None)
+
+    def bwd(x=P, ty=0, ld=100, N=3, V=100, t=P, stats=P, g=P, c=1.0, grad=2 * P, ldg=100):
+        return csv.lib.csv_token_logprobs_backward(x, ty, ld, N, V, t, stats, g, c, grad, ldg, None)
+
+    def pol(x=P, ty=0, ld=100, N=3, V=100, t=P, old=P, ref=P, adv=P, w=P, lo=0.2, hi=0.2, beta=0.1, c=1.0, loss=P, logp=P, grad=2 * P, ldg=100,
+            scr=P, size=big, params=True):
+        p = csv.PolicyParams(lo, hi, beta, c)
+        return csv.lib.csv_policy_loss(x, ty, ld, N, V, t, old, ref, adv, w, C.byref(p) if params else None, loss, logp, grad, ldg, scr, size, None)
+
+    for f in (fwd, bwd, pol):
+        assert f(N=-1) == ESHAPE
+        assert f(V=0) == ESHAPE
+        assert f(ld=99) == ESHAPE
+        assert f(ty=7) == EINVAL
+        assert f(x=None) == EINVAL
+        assert f(t=None) == EINVAL
+        assert f(x=P + 2) == EINVAL                                # float32 at an odd half
+        for c in (0.0, -1.0, float("nan"), float("inf"), 3e38):
+            assert f(c=c) == EINVAL
+    for f in (fwd, pol):
+        assert f(scr=None) == ESHAPE
+        assert f(size=8) == ESHAPE
+        assert f(scr=P + 8) == EINVAL
+    assert fwd(logp=None) == EINVAL and fwd(stats=None) == EINVAL
+    assert fwd(x=None, t=None, N=0, logp=None, stats=None, scr=None, size=0) == 0
+    for f in (bwd, pol):
+        assert f(ldg=99) == ESHAPE
+        assert f(grad=2 * P + 2) == EINVAL
+        assert f(grad=P, ldg=104) == EINVAL                        # in place, other rows
+    assert bwd(stats=None) == EINVAL and bwd(g=None) == EINVAL and bwd(grad=None) == EINVAL
+    assert bwd(x=None, t=None, N=0, stats=None, g=None, grad=None) == 0
+    assert pol(params=False) == EINVAL and pol(loss=None) == EINVAL
+    for bad in (dict(lo=-0.1), dict(lo=1.5), dict(hi=-0.1), dict(hi=float("nan")), dict(beta=-1.0), dict(beta=float("inf")), dict(beta=float("nan")),
+                dict(ref=None), dict(old=None), dict(adv=None), dict(w=None)):
+        assert pol(**bad) == EINVAL, bad
+
+
+def test_binding_refuses_host_tensors_and_wrong_types(csv):
+    x = torch.zeros(4, 64)
+    with pytest.raises(ValueError):
+        csv.csv_mx4_quantize(x)
+    with pytest.raises(ValueError):
+        csv.csv_mx4_quantize(x.half())
+    with pytest.raises(ValueError):
+        csv.csv_mx4_quantize(x.t())
+    with pytest.raises(ValueError):
+        csv.csv_token_logprobs(x, torch.zeros(4, dtype=torch.int32))
+    with pytest.raises(ValueError):
+        csv.csv_policy_loss(x.double(), None, None, None, None, None)
+    assert csv.mx4_padded(1) == 128 and csv.mx4_padded(128) == 128 and csv.mx4_padded(136) == 256
+
+
+def test_policy_formula_against_differences():
+    """The derivative that the kernels are held to, against central differences of the loss in float64, away from the borders of the clip."""
+    from . import _operators as O
+    rng = np.random.default_rng(3)
+    N, V, c = 12, 23, 1.3
+    x = rng.normal(size=(N, V)) * 2
+    t = rng.integers(0, V, N)
+    logp = O.rows_logp(x, t, c)[2]
+    ratio = rng.choice([0.5, 0.7, 0.9, 1.1, 1.5], N)               # borders at 0.8 and 1.28
+    old, ref = logp - np.log(ratio), logp + rng.normal(size=N) * 0.4
+    adv, w = rng.normal(size=N), rng.uniform(0.1, 1, N)
+
+    def loss(x):
+        return O.policy(O.rows_logp(x, t, c)[2], old, ref, adv, w, 0.2, 0.28, 0.3)[0].sum()
+
+    m, s, lp, p = O.rows_logp(x, t, c)
+    g = O.grad_rows(p, s, t, O.policy(lp, old, ref, adv, w, 0.2, 0.28, 0.3)[1], c)
+    h = 1e-5
+    for i in range(N):
+        for j in rng.integers(0, V, 4).tolist() + [int(t[i])]:
+            xp, xm = x.copy(), x.copy()
+            xp[i, j] += h
+            xm[i, j] -= h
+            # second differences of the loss are below 40: h^2 times that, and the cancellation of values near 1
+            assert abs((loss(xp) - loss(xm)) / (2 * h) - g[i, j]) < 40 * h * h + 1e-10

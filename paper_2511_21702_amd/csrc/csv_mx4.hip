@@ -3,7 +3,7 @@
 //   quantize_kernel     blocks of 32 elements -> one scale byte and 32 four-bit codes, row-major or in matrix-core tiles
 //   dequantize_kernel   the values that row-major codes stand for
 //   lay_out_kernel      row-major codes of a head -> tiles
-//   logits_kernel       out[b, i] = <W_i, h_b> + b_i on the matrix cores
+//   product_kernel      out[b, i] = <W_i, h_b> + b_i on the matrix cores
 //
 // A tile is 16 rows x 128 elements: lane l of a wave holds the 32 elements of block l / 16 of row l % 16 (16 bytes) and that
 // block's scale, which is how v_mfma_scale_f32_16x16x128_f8f6f4 takes an operand.  Codes of a tile are 1 KB in lane order; the
@@ -16,6 +16,7 @@
 #define CHUNK 128     // elements of a row in a tile; rows are padded to a multiple of it
 #define HEAD_ROWS 256 // rows of a head are padded to a multiple of it (with codes 0), so that no product kernel tests a row before it stores
 
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v2f __attribute__((ext_vector_type(2)));
@@ -143,58 +144,214 @@ struct LogitsArgs {
     const uint32_t* scales;
     const float* bias;
     int V, d, chunks, B;
+    int blocks;                 // blocks of rows
+    int groups;                 // blocks of hidden states
     const uint16_t* h;          // bf16 [B, d]
     const uint8_t* hc;          // or 4-bit tiles of it
     const uint32_t* hs;
     void* out;
+    int wide;                   // rows of the output are 16-byte aligned
 };
 
-__device__ __forceinline__ v8i widen(const uint4& u) { return v8i{(int)u.x, (int)u.y, (int)u.z, (int)u.w, 0, 0, 0, 0}; }
+__device__ __forceinline__ v8i widen(const v4u& u) { return v8i{(int)u.x, (int)u.y, (int)u.z, (int)u.w, 0, 0, 0, 0}; }
 __device__ __forceinline__ v8bf bf16_of_fp4(uint32_t c, float s) {
     const v2bf a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1),
                e = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2), f = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3);
     return v8bf{a[0], a[1], b[0], b[1], e[0], e[1], f[0], f[1]};
 }
-__device__ __forceinline__ void store1(float* p, float v) { *p = v; }
-__device__ __forceinline__ void store1(uint16_t* p, float v) { *p = __builtin_bit_cast(uint16_t, (__bf16)v); }
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)a) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)b) << 16;
+}
 
-// One wave: 16 rows x 16 hidden states.  The sum over k runs in the order of the storage, so both forms of the second operand put element
-// 32 (l / 16) + 8 s + j of a tile at lane l: a 4-bit tile goes to one matrix instruction as it is, against bf16 it is widened (exactly)
-// to four operands s = 0..3 of 16x16x32.
-template <bool MX4, typename T>
-__global__ __launch_bounds__(256) void logits_kernel(LogitsArgs a) {
-    const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
-    const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int quads = (a.chunks + 3) >> 2;
-    const uint8_t* wc = a.codes + tile * a.chunks * 1024 + lane * 16;
-    const uint32_t* ws = a.scales + tile * quads * 64 + lane;
-    const int b = blockIdx.y * 16 + col;
-    v4f acc = {0.f, 0.f, 0.f, 0.f};
-    for (int c = 0; c < a.chunks; ++c) {
-        const uint4 w = *(const uint4*)(wc + (int64_t)c * 1024);
-        const uint32_t s = ws[(c >> 2) * 64] >> (8 * (c & 3)) & 255u;
-        if (MX4) {
-            const int64_t ht = (int64_t)blockIdx.y * a.chunks + c;
-            const uint4 x = *(const uint4*)(a.hc + ht * 1024 + lane * 16);
-            const uint32_t xs = a.hs[((int64_t)blockIdx.y * quads + (c >> 2)) * 64 + lane] >> (8 * (c & 3)) & 255u;
-            acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widen(w), widen(x), acc, 4, 4, 0, s, 0, xs);
-        } else {
-            const float sf = __uint_as_float(s << 23);
-            const uint32_t q[4] = {w.x, w.y, w.z, w.w};
-            for (int k = 0; k < 4; ++k) {
-                const int e = c * CHUNK + g * BLK + k * 8;
-                uint4 x = make_uint4(0, 0, 0, 0);
-                if (b < a.B && e < a.d) x = *(const uint4*)(a.h + (int64_t)b * a.d + e);
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of_fp4(q[k], sf), __builtin_bit_cast(v8bf, x), acc, 0, 0, 0);
+// Waits for the wave's LDS traffic only: requests to global memory stay in flight across the barrier.
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// Four waves, RT tiles of 16 rows each, against NT groups of 16 hidden states; K goes by in stages of S tiles of 128.
+//
+// The sum over k may run in any order that both operands share.  A tile puts element 32 (l / 16) + 8 s + j at lane l, so a 4-bit tile goes to
+// one 16x16x128 instruction as it is, and against bf16 it is widened (exactly) to four operands s = 0..3 of 16x16x32.
+// Codes of W are read once, straight into registers, a stage ahead: a register is requested again as soon as its products are issued.  The
+// stage of h lies in LDS, two buffers, and passes through registers on its way there, so that a barrier waits for no load.  bf16 h lies row by
+// row with the 16-byte pieces of row t exchanged by t % 16 (a column of pieces then spreads over all banks); 4-bit h lies as its tiles.
+// Past the end of a row or of the batch the last piece or row is read again: codes of W are 0 there, and those hidden states are not stored.
+template <bool MX4, int NT, int RT, int S, typename T>
+__global__ __launch_bounds__(256, NT == 8 ? 2 : 3) void product_kernel(LogitsArgs a) {
+    constexpr int HP = NT * S * (MX4 ? 64 : 256);                 // 16-byte pieces of a stage of h
+    constexpr int HT = (HP + 255) / 256;                          // of them per thread
+    constexpr int OW = RT * 16 + 4;                               // floats per hidden state in a wave's part of the output buffer
+    constexpr int LDS = 2 * HP > 4 * 16 * OW / 4 ? 2 * HP : 4 * 16 * OW / 4;
+    __shared__ v4u lds[LDS];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, col = lane & 15;
+    // blocks of one die (every eighth) take the groups of hidden states of one block of rows after each other: W comes from that die's cache
+    const int j = blockIdx.x >> 3, group = j % a.groups, block = (j / a.groups) * 8 + (blockIdx.x & 7);
+    if (block >= a.blocks) return;
+    const int chunks = a.chunks, quads = (chunks + 3) >> 2, stages = (chunks + S - 1) / S;
+    const int64_t tile0 = (int64_t)block * (4 * RT) + wave * RT;
+    const v4u* wc = (const v4u*)a.codes + tile0 * chunks * 64 + lane;
+    const uint32_t* ws = a.scales + tile0 * quads * 64 + lane;
+    const int64_t htile0 = (int64_t)group * NT;
+    const uint32_t* hs = MX4 ? a.hs + htile0 * quads * 64 + lane : nullptr;
+
+    v4u w[S][RT], hr[HT];
+    uint32_t sw[RT], sh[MX4 ? NT : 1], sw_next[RT], sh_next[MX4 ? NT : 1];
+    auto load_w = [&](int c, v4u (&to)[RT]) {
+        const int cc = min(c, chunks - 1);
+        #pragma unroll
+        for (int r = 0; r < RT; ++r) to[r] = wc[((int64_t)r * chunks + cc) * 64];
+    };
+    auto load_scales = [&](int c0) {                              // a stage lies within four tiles
+        const int q = min(c0, chunks - 1) >> 2;
+        #pragma unroll
+        for (int r = 0; r < RT; ++r) sw_next[r] = ws[((int64_t)r * quads + q) * 64];
+        if (MX4)
+            #pragma unroll
+            for (int n = 0; n < NT; ++n) sh_next[n] = hs[((int64_t)n * quads + q) * 64];
+    };
+    auto load_h = [&](int c0) {
+        #pragma unroll
+        for (int i = 0; i < HT; ++i) {
+            const int p = tid + i * 256;
+            if (HP % 256 != 0 && p >= HP) continue;
+            if (MX4) {
+                const int c = p / (NT * 64), n = p / 64 % NT;
+                hr[i] = ((const v4u*)a.hc)[((htile0 + n) * chunks + min(c0 + c, chunks - 1)) * 64 + (p & 63)];
+            } else {
+                const int c = p / (NT * 256), t = p / 16 % (NT * 16);
+                const int64_t b = min((int)(htile0 * 16) + t, a.B - 1);
+                hr[i] = *(const v4u*)(a.h + b * a.d + min((c0 + c) * CHUNK + (p & 15) * 8, a.d - 8));
             }
         }
+    };
+    auto store_h = [&](int buf) {
+        #pragma unroll
+        for (int i = 0; i < HT; ++i) {
+            const int p = tid + i * 256;
+            if (HP % 256 != 0 && p >= HP) continue;
+            lds[buf * HP + (MX4 ? p : p ^ (p >> 4 & 15))] = hr[i];
+        }
+    };
+    v4f acc[RT][NT];
+    #pragma unroll
+    for (int r = 0; r < RT; ++r)
+        #pragma unroll
+        for (int n = 0; n < NT; ++n) acc[r][n] = v4f{0.f, 0.f, 0.f, 0.f};
+    auto products = [&](int buf, int c, const v4u (&x)[RT]) {
+        const v4u* hb = lds + buf * HP + c * NT * (MX4 ? 64 : 256);
+        if (MX4) {
+            #pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const v4u y = hb[n * 64 + lane];
+                #pragma unroll
+                for (int r = 0; r < RT; ++r)
+                    acc[r][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widen(x[r]), widen(y), acc[r][n], 4, 4, 0, sw[r] >> (8 * c), 0, sh[n] >> (8 * c));
+            }
+        } else {
+            #pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                v8bf wide[RT];
+                #pragma unroll
+                for (int r = 0; r < RT; ++r) wide[r] = bf16_of_fp4(x[r][s], __uint_as_float((sw[r] >> (8 * c) & 255u) << 23));
+                #pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const v8bf y = __builtin_bit_cast(v8bf, hb[(n * 16 + col) * 16 + ((4 * g + s) ^ col)]);
+                    #pragma unroll
+                    for (int r = 0; r < RT; ++r) acc[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide[r], y, acc[r][n], 0, 0, 0);
+                }
+            }
+        }
+    };
+    auto take_scales = [&](int c0) {
+        #pragma unroll
+        for (int r = 0; r < RT; ++r) sw[r] = sw_next[r] >> (8 * (c0 & 3));
+        if (MX4)
+            #pragma unroll
+            for (int n = 0; n < NT; ++n) sh[n] = sh_next[n] >> (8 * (c0 & 3));
+    };
+
+    load_h(0);
+    load_scales(0);
+    #pragma unroll
+    for (int c = 0; c < S; ++c) load_w(c, w[c]);
+    for (int st = 0; st < stages - 1; ++st) {
+        store_h(st & 1);
+        take_scales(st * S);
+        load_h((st + 1) * S);
+        load_scales((st + 1) * S);
+        lds_barrier();
+        #pragma unroll
+        for (int c = 0; c < S; ++c) {
+            products(st & 1, c, w[c]);
+            load_w((st + 1) * S + c, w[c]);
+        }
     }
-    if (b >= a.B) return;
-    T* out = (T*)a.out + (int64_t)b * a.V;
-    for (int r = 0; r < 4; ++r) {
-        const int64_t row = tile * 16 + g * 4 + r;
-        if (row < a.V) store1(out + row, acc[r] + (a.bias ? a.bias[row] : 0.f));
+    const int last = stages - 1;                                  // the last stage asks for nothing more
+    store_h(last & 1);
+    take_scales(last * S);
+    lds_barrier();
+    #pragma unroll
+    for (int c = 0; c < S; ++c)
+        if (last * S + c < chunks) products(last & 1, c, w[c]);
+
+    // Output: lane l holds rows 4 (l / 16) .. + 3 of hidden state l % 16 of every tile.  Through LDS, 16 hidden states at a time, so that a row of
+    // logits is written in one piece per wave.
+    __syncthreads();
+    float* buf = (float*)lds + wave * 16 * OW;
+    const int64_t row0 = tile0 * 16;
+    #pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int64_t b0 = (htile0 + n) * 16;
+        if (b0 >= a.B) continue;
+        #pragma unroll
+        for (int r = 0; r < RT; ++r) *(v4f*)(buf + col * OW + r * 16 + g * 4) = acc[r][n];
+        __builtin_amdgcn_wave_barrier();
+        constexpr int W = sizeof(T) == 4 ? 4 : 8;                 // logits in 16 bytes
+        if (a.wide) {
+            constexpr int L = RT * 16 / W;                        // lanes of a hidden state
+            const int64_t row = row0 + lane % L * W;
+            if (row < a.V) {
+                float bias[W];
+                #pragma unroll
+                for (int i = 0; i < W; ++i) bias[i] = a.bias ? a.bias[row + i] : 0.f;
+                for (int t = lane / L; t < 16 && b0 + t < a.B; t += 64 / L) {
+                    float v[W];
+                    #pragma unroll
+                    for (int i = 0; i < W; ++i) v[i] = buf[t * OW + lane % L * W + i] + bias[i];
+                    T* to = (T*)a.out + (b0 + t) * a.V + row;
+                    if constexpr (sizeof(T) == 4) *(float4*)to = make_float4(v[0], v[1], v[2], v[3]);
+                    else *(v4u*)to = v4u{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+                }
+            }
+        } else {
+            constexpr int L = RT * 16;
+            const int64_t row = row0 + lane % L;
+            if (row < a.V) {
+                const float bias = a.bias ? a.bias[row] : 0.f;
+                for (int t = lane / L; t < 16 && b0 + t < a.B; t += 64 / L) {
+                    const float v = buf[t * OW + lane % L] + bias;
+                    T* to = (T*)a.out + (b0 + t) * a.V + row;
+                    if constexpr (sizeof(T) == 4) *to = v;
+                    else *to = __builtin_bit_cast(uint16_t, (__bf16)v);
+                }
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
     }
+}
+
+template <bool MX4, int NT, int RT, int S>
+static int launch_product(LogitsArgs a, int out_type, hipStream_t st) {
+    a.blocks = (a.V + 64 * RT - 1) / (64 * RT);
+    a.groups = (a.B + NT * 16 - 1) / (NT * 16);
+    const int64_t n = (int64_t)(a.blocks + 7) / 8 * 8 * a.groups;
+    if (n > 0x7fffffff) { csv_set_error("V=%d rows x B=%d hidden states are too many blocks", a.V, a.B); return CSV_ESHAPE; }
+    if (out_type == CSV_F32) product_kernel<MX4, NT, RT, S, float><<<(unsigned)n, 256, 0, st>>>(a);
+    else product_kernel<MX4, NT, RT, S, uint16_t><<<(unsigned)n, 256, 0, st>>>(a);
+    CSV_LAUNCH_CHECK("product_kernel");
+    return CSV_OK;
 }
 
 // ------------------------------------------------------------------------------------------------ entry points
@@ -290,14 +447,18 @@ static int check_logits(const csv_mx4_head* x, int B, int act) {
     if (act != CSV_ACT_BF16 && act != CSV_ACT_MX4) { csv_set_error("bad act=%d", act); return CSV_EINVAL; }
     return CSV_OK;
 }
-// rows of the 4-bit copy of h: whole tiles
-static inline int64_t tiles16(int B) { return ((int64_t)B + 15) / 16; }
+// groups of 16 hidden states that a block of the product takes together, and tiles of the 4-bit copy of h: whole blocks
+static inline int groups_of(int B) { return B <= 16 ? 1 : B <= 32 ? 2 : B <= 64 ? 4 : 8; }
+static inline int64_t tiles_of(int B) {
+    const int64_t nt = groups_of(B);
+    return ((int64_t)B + 16 * nt - 1) / (16 * nt) * nt;
+}
 
 extern "C" int csv_mx4_logits_scratch(const csv_mx4_head* x, int B, int act, size_t* bytes) {
     const int rc = check_logits(x, B, act);
     if (rc) return rc;
     if (!bytes) { csv_set_error("null bytes"); return CSV_EINVAL; }
-    *bytes = act == CSV_ACT_BF16 ? 0 : (size_t)tiles16(B) * ((size_t)x->chunks * 1024 + (size_t)((x->chunks + 3) / 4) * 256);
+    *bytes = act == CSV_ACT_BF16 ? 0 : (size_t)tiles_of(B) * ((size_t)x->chunks * 1024 + (size_t)((x->chunks + 3) / 4) * 256);
     return CSV_OK;
 }
 
@@ -317,8 +478,10 @@ extern "C" int csv_mx4_logits(const csv_mx4_head* x, const uint16_t* d_h, int B,
     CSV_HIP(hipGetDevice(&dev));
     if (dev != x->device) { csv_set_error("the head lives on device %d, the current device is %d", x->device, dev); return CSV_EINVAL; }
     const hipStream_t st = (hipStream_t)stream;
-    LogitsArgs a = {x->codes, x->scales, x->bias, x->V, x->d, x->chunks, B, d_h, nullptr, nullptr, d_logits};
-    const int64_t tt = tiles16(B);
+    LogitsArgs a = {};
+    a.codes = x->codes; a.scales = x->scales; a.bias = x->bias; a.V = x->V; a.d = x->d; a.chunks = x->chunks; a.B = B; a.h = d_h; a.out = d_logits;
+    a.wide = ((uintptr_t)d_logits & 15) == 0 && x->V % (out_type == CSV_F32 ? 4 : 8) == 0;
+    const int64_t tt = tiles_of(B);
     if (act == CSV_ACT_MX4) {
         uint8_t* hc = (uint8_t*)d_scratch;
         uint8_t* hs = hc + (size_t)tt * x->chunks * 1024;
@@ -327,14 +490,14 @@ extern "C" int csv_mx4_logits(const csv_mx4_head* x, const uint16_t* d_h, int B,
         a.hc = hc;
         a.hs = (const uint32_t*)hs;
     }
-    const dim3 g((unsigned)((x->V + 63) / 64), (unsigned)tt);
-    if (act == CSV_ACT_MX4) {
-        if (out_type == CSV_F32) logits_kernel<true, float><<<g, 256, 0, st>>>(a);
-        else logits_kernel<true, uint16_t><<<g, 256, 0, st>>>(a);
-    } else {
-        if (out_type == CSV_F32) logits_kernel<false, float><<<g, 256, 0, st>>>(a);
-        else logits_kernel<false, uint16_t><<<g, 256, 0, st>>>(a);
+    switch (groups_of(B) * 2 + act) {
+        case 2: return launch_product<false, 1, 2, 4>(a, out_type, st);
+        case 3: return launch_product<true, 1, 2, 4>(a, out_type, st);
+        case 4: return launch_product<false, 2, 2, 2>(a, out_type, st);
+        case 5: return launch_product<true, 2, 2, 4>(a, out_type, st);
+        case 8: return launch_product<false, 4, 4, 1>(a, out_type, st);
+        case 9: return launch_product<true, 4, 4, 2>(a, out_type, st);
+        case 16: return launch_product<false, 8, 4, 1>(a, out_type, st);
+        default: return launch_product<true, 8, 4, 2>(a, out_type, st);
     }
-    CSV_LAUNCH_CHECK("logits_kernel");
-    return CSV_OK;
 }

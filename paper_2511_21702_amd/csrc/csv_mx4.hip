@@ -8,6 +8,9 @@
 // A tile is 16 rows x 128 elements: lane l of a wave holds the 32 elements of block l / 16 of row l % 16 (16 bytes) and that
 // block's scale, which is how v_mfma_scale_f32_16x16x128_f8f6f4 takes an operand.  Codes of a tile are 1 KB in lane order; the
 // scales of four tiles that follow each other along the row are one dword per lane, byte c for tile c.
+// A head is cut into bands of 64 rows.  A band is one piece of memory in the order in which it is read: for every four steps of 128
+// elements the scales of its four tiles (1 KB), then for each step the codes of its four tiles (4 KB).  Bands are no power of two apart,
+// so that blocks that start together do not ask for the same memory channels.
 #include "csv_common.h"
 
 #include <stdlib.h>
@@ -19,6 +22,7 @@
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
 typedef float v2f __attribute__((ext_vector_type(2)));
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
@@ -26,12 +30,15 @@ typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 struct csv_mx4_head {
     int V, d, device;
     int chunks;         // tiles along a row
-    uint8_t* codes;     // [rows16 / 16][chunks][1024]
-    uint32_t* scales;   // [rows16 / 16][(chunks + 3) / 4][64]
+    uint8_t* bands;     // [rows / 64][band_bytes(chunks)]
     float* bias;        // [V] or NULL
 };
 
 static inline int chunks_of(int d) { return (d + CHUNK - 1) / CHUNK; }
+__host__ __device__ static inline int64_t band_bytes(int chunks) { return (int64_t)((chunks + 3) >> 2) * 1024 + (int64_t)chunks * 4096; }
+// bytes from the start of a band to the scales of steps 4q .. 4q + 3, and to the codes of step c
+__host__ __device__ static inline int64_t scales_at(int q) { return (int64_t)q * (1024 + 4 * 4096); }
+__host__ __device__ static inline int64_t codes_at(int c) { return (int64_t)c * 4096 + ((c >> 2) + 1) * 1024; }
 
 // ------------------------------------------------------------------------------------------------ rounding
 // Eight elements of a lane; four lanes hold a block.  The scale is taken from the exponent field of the largest magnitude alone:
@@ -112,15 +119,16 @@ __global__ __launch_bounds__(256) void dequantize_kernel(const uint8_t* __restri
     }
 }
 
-// One thread: 16 bytes of a tile, and where it is the first tile of four a dword of scales.  What the padding of a row holds is not taken over.
+// One thread: 16 bytes of a tile, and at the first of four steps a dword of scales.  What the padding of a row holds is not taken over.
 __global__ __launch_bounds__(256) void lay_out_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int V, int d, int chunks, int64_t pieces,
-                                                       uint8_t* __restrict__ to, uint32_t* __restrict__ to_scales) {
+                                                       uint8_t* __restrict__ bands) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= pieces) return;
-    const int l = (int)(i & 63), g = l >> 4;
-    const int64_t t = i >> 6;
+    const int l = (int)(i & 63), g = l >> 4, tile = (int)(i >> 6) & 3;
+    const int64_t t = i >> 8;
     const int chunk = (int)(t % chunks);
-    const int64_t tile = t / chunks, row = tile * 16 + (l & 15);
+    const int64_t band = t / chunks, row = band * 64 + tile * 16 + (l & 15);
+    uint8_t* to = bands + band * band_bytes(chunks);
     uint4 c = make_uint4(0, 0, 0, 0);
     const int left = d - chunk * CHUNK - g * BLK;      // elements of the row from this block on, a multiple of 8
     if (row < V && left > 0) {
@@ -129,19 +137,18 @@ __global__ __launch_bounds__(256) void lay_out_kernel(const uint8_t* __restrict_
         if (left <= 16) c.z = 0;
         if (left <= 8) c.y = 0;
     }
-    *(uint4*)(to + i * 16) = c;
+    *(uint4*)(to + codes_at(chunk) + tile * 1024 + l * 16) = c;
     if ((chunk & 3) == 0) {
         uint32_t s = 0;
         for (int k = 0; k < 4; ++k)
             if (row < V && left > k * CHUNK) s |= (uint32_t)scales[(row * chunks + chunk + k) * 4 + g] << (8 * k);
-        to_scales[(tile * ((chunks + 3) >> 2) + (chunk >> 2)) * 64 + l] = s;
+        *(uint32_t*)(to + scales_at(chunk >> 2) + tile * 256 + l * 4) = s;
     }
 }
 
 // ------------------------------------------------------------------------------------------------ product
 struct LogitsArgs {
-    const uint8_t* codes;
-    const uint32_t* scales;
+    const uint8_t* bands;
     const float* bias;
     int V, d, chunks, B;
     int blocks;                 // blocks of rows
@@ -178,12 +185,18 @@ __device__ __forceinline__ void lds_barrier() {
 // stage of h lies in LDS, two buffers, and passes through registers on its way there, so that a barrier waits for no load.  bf16 h lies row by
 // row with the 16-byte pieces of row t exchanged by t % 16 (a column of pieces then spreads over all banks); 4-bit h lies as its tiles.
 // Past the end of a row or of the batch the last piece or row is read again: codes of W are 0 there, and those hidden states are not stored.
+// With many hidden states in four bits the product is bound by the matrix cores, and 32x32x64 instructions run at 1.7 times the rate of
+// 16x16x128 (6.6 and 3.85 PFLOP/s measured on registers alone).  Lane l of theirs holds a block of row l % 32: two tiles side by side, read
+// in pieces of 256 bytes, blocks l / 32 and then 2 + l / 32 of a step.
 template <bool MX4, int NT, int RT, int S, typename T>
 __global__ __launch_bounds__(256, NT == 8 ? 2 : 3) void product_kernel(LogitsArgs a) {
     constexpr int HP = NT * S * (MX4 ? 64 : 256);                 // 16-byte pieces of a stage of h
     constexpr int HT = (HP + 255) / 256;                          // of them per thread
+    constexpr bool BIG = MX4 && NT == 8;                          // 32x32x64 instructions
+    constexpr int G = BIG ? 32 : 16;                              // hidden states of an instruction
     constexpr int OW = RT * 16 + 4;                               // floats per hidden state in a wave's part of the output buffer
-    constexpr int LDS = 2 * HP > 4 * 16 * OW / 4 ? 2 * HP : 4 * 16 * OW / 4;
+    constexpr int LDS = 2 * HP > 4 * G * OW / 4 ? 2 * HP : 4 * G * OW / 4;
+    static_assert(!BIG || RT == 4, "a wave takes whole bands");
     __shared__ v4u lds[LDS];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, col = lane & 15;
     // blocks of one die (every eighth) take the groups of hidden states of one block of rows after each other: W comes from that die's cache
@@ -191,28 +204,34 @@ __global__ __launch_bounds__(256, NT == 8 ? 2 : 3) void product_kernel(LogitsArg
     if (block >= a.blocks) return;
     const int chunks = a.chunks, quads = (chunks + 3) >> 2, stages = (chunks + S - 1) / S;
     const int64_t tile0 = (int64_t)block * (4 * RT) + wave * RT;
-    const v4u* wc = (const v4u*)a.codes + tile0 * chunks * 64 + lane;
-    const uint32_t* ws = a.scales + tile0 * quads * 64 + lane;
+    const uint8_t* band = a.bands + (tile0 >> 2) * band_bytes(chunks);
+    // where in a run of 64-lane tiles this lane's block is, in lanes; registers r of a step are r tiles on, or (BIG) tiles 2 (r / 2), blocks 2 (r % 2)
+    const int at = BIG ? (lane >> 4 & 1) * 64 + (lane >> 5) * 16 + col : lane;
+    auto step = [](int r) { return BIG ? (r >> 1) * 128 + (r & 1) * 32 : r * 64; };
+    const uint8_t *wc = band + (tile0 & 3) * 1024 + at * 16, *ws = band + (tile0 & 3) * 256 + at * 4;
     const int64_t htile0 = (int64_t)group * NT;
-    const uint32_t* hs = MX4 ? a.hs + htile0 * quads * 64 + lane : nullptr;
+    const uint32_t* hs = MX4 ? a.hs + htile0 * quads * 64 : nullptr;
 
     v4u w[S][RT], hr[HT];
     uint32_t sw[RT], sh[MX4 ? NT : 1], sw_next[RT], sh_next[MX4 ? NT : 1];
     auto load_w = [&](int c, v4u (&to)[RT]) {
         const int cc = min(c, chunks - 1);
-        #pragma unroll
-        for (int r = 0; r < RT; ++r) to[r] = wc[((int64_t)r * chunks + cc) * 64];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) to[r] = *(const v4u*)(wc + codes_at(cc) + step(r) * 16);
     };
     auto load_scales = [&](int c0) {                              // a stage lies within four tiles
         const int q = min(c0, chunks - 1) >> 2;
-        #pragma unroll
-        for (int r = 0; r < RT; ++r) sw_next[r] = ws[((int64_t)r * quads + q) * 64];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) sw_next[r] = *(const uint32_t*)(ws + scales_at(q) + step(r) * 4);
         if (MX4)
-            #pragma unroll
-            for (int n = 0; n < NT; ++n) sh_next[n] = hs[((int64_t)n * quads + q) * 64];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const int i = at + step(n);                      // tile i / 64
+                sh_next[n] = hs[((int64_t)(i >> 6) * quads + q) * 64 + (i & 63)];
+            }
     };
     auto load_h = [&](int c0) {
-        #pragma unroll
+#pragma unroll
         for (int i = 0; i < HT; ++i) {
             const int p = tid + i * 256;
             if (HP % 256 != 0 && p >= HP) continue;
@@ -227,54 +246,69 @@ __global__ __launch_bounds__(256, NT == 8 ? 2 : 3) void product_kernel(LogitsArg
         }
     };
     auto store_h = [&](int buf) {
-        #pragma unroll
+#pragma unroll
         for (int i = 0; i < HT; ++i) {
             const int p = tid + i * 256;
             if (HP % 256 != 0 && p >= HP) continue;
             lds[buf * HP + (MX4 ? p : p ^ (p >> 4 & 15))] = hr[i];
         }
     };
-    v4f acc[RT][NT];
-    #pragma unroll
-    for (int r = 0; r < RT; ++r)
-        #pragma unroll
-        for (int n = 0; n < NT; ++n) acc[r][n] = v4f{0.f, 0.f, 0.f, 0.f};
+    v16f big[BIG ? 2 : 1][BIG ? 4 : 1];
+#pragma unroll
+    for (int r = 0; r < (BIG ? 2 : 1); ++r)
+#pragma unroll
+        for (int n = 0; n < (BIG ? 4 : 1); ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) big[r][n][i] = 0.f;
+    v4f acc[BIG ? 1 : RT][BIG ? 1 : NT];
+#pragma unroll
+    for (int r = 0; r < (BIG ? 1 : RT); ++r)
+#pragma unroll
+        for (int n = 0; n < (BIG ? 1 : NT); ++n) acc[r][n] = v4f{0.f, 0.f, 0.f, 0.f};
     auto products = [&](int buf, int c, const v4u (&x)[RT]) {
         const v4u* hb = lds + buf * HP + c * NT * (MX4 ? 64 : 256);
-        if (MX4) {
-            #pragma unroll
+        if constexpr (BIG) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const v4u y = hb[at + step(n)];
+#pragma unroll
+                for (int r = n & 1; r < RT; r += 2)
+                    big[r >> 1][n >> 1] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(widen(x[r]), widen(y), big[r >> 1][n >> 1], 4, 4, 0, sw[r] >> (8 * c), 0, sh[n] >> (8 * c));
+            }
+        } else if constexpr (MX4) {
+#pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const v4u y = hb[n * 64 + lane];
-                #pragma unroll
+#pragma unroll
                 for (int r = 0; r < RT; ++r)
                     acc[r][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widen(x[r]), widen(y), acc[r][n], 4, 4, 0, sw[r] >> (8 * c), 0, sh[n] >> (8 * c));
             }
         } else {
-            #pragma unroll
+#pragma unroll
             for (int s = 0; s < 4; ++s) {
                 v8bf wide[RT];
-                #pragma unroll
+#pragma unroll
                 for (int r = 0; r < RT; ++r) wide[r] = bf16_of_fp4(x[r][s], __uint_as_float((sw[r] >> (8 * c) & 255u) << 23));
-                #pragma unroll
+#pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     const v8bf y = __builtin_bit_cast(v8bf, hb[(n * 16 + col) * 16 + ((4 * g + s) ^ col)]);
-                    #pragma unroll
+#pragma unroll
                     for (int r = 0; r < RT; ++r) acc[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide[r], y, acc[r][n], 0, 0, 0);
                 }
             }
         }
     };
     auto take_scales = [&](int c0) {
-        #pragma unroll
+#pragma unroll
         for (int r = 0; r < RT; ++r) sw[r] = sw_next[r] >> (8 * (c0 & 3));
         if (MX4)
-            #pragma unroll
+#pragma unroll
             for (int n = 0; n < NT; ++n) sh[n] = sh_next[n] >> (8 * (c0 & 3));
     };
 
     load_h(0);
     load_scales(0);
-    #pragma unroll
+#pragma unroll
     for (int c = 0; c < S; ++c) load_w(c, w[c]);
     for (int st = 0; st < stages - 1; ++st) {
         store_h(st & 1);
@@ -282,31 +316,40 @@ __global__ __launch_bounds__(256, NT == 8 ? 2 : 3) void product_kernel(LogitsArg
         load_h((st + 1) * S);
         load_scales((st + 1) * S);
         lds_barrier();
-        #pragma unroll
+#pragma unroll
         for (int c = 0; c < S; ++c) {
             products(st & 1, c, w[c]);
             load_w((st + 1) * S + c, w[c]);
+            __builtin_amdgcn_sched_barrier(0);                    // requests stay where they are written
         }
     }
     const int last = stages - 1;                                  // the last stage asks for nothing more
     store_h(last & 1);
     take_scales(last * S);
     lds_barrier();
-    #pragma unroll
+#pragma unroll
     for (int c = 0; c < S; ++c)
         if (last * S + c < chunks) products(last & 1, c, w[c]);
 
-    // Output: lane l holds rows 4 (l / 16) .. + 3 of hidden state l % 16 of every tile.  Through LDS, 16 hidden states at a time, so that a row of
-    // logits is written in one piece per wave.
+    // Output: lane l holds rows 4 (l / 16) .. + 3 of hidden state l % 16 of every tile, or rows 8 i + 4 (l / 32) .. + 3 of hidden state l % 32.
+    // Through LDS, 16 or 32 hidden states at a time, so that a row of logits is written in one piece per wave.
     __syncthreads();
-    float* buf = (float*)lds + wave * 16 * OW;
+    float* buf = (float*)lds + wave * G * OW;
     const int64_t row0 = tile0 * 16;
-    #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int64_t b0 = (htile0 + n) * 16;
+#pragma unroll
+    for (int n = 0; n < NT * 16 / G; ++n) {
+        const int64_t b0 = htile0 * 16 + n * G;
         if (b0 >= a.B) continue;
-        #pragma unroll
-        for (int r = 0; r < RT; ++r) *(v4f*)(buf + col * OW + r * 16 + g * 4) = acc[r][n];
+        if constexpr (BIG) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    *(v4f*)(buf + (lane & 31) * OW + r * 32 + i * 8 + (lane >> 5) * 4) = v4f{big[r][n][4 * i], big[r][n][4 * i + 1], big[r][n][4 * i + 2], big[r][n][4 * i + 3]};
+        } else {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) *(v4f*)(buf + col * OW + r * 16 + g * 4) = acc[r][n];
+        }
         __builtin_amdgcn_wave_barrier();
         constexpr int W = sizeof(T) == 4 ? 4 : 8;                 // logits in 16 bytes
         if (a.wide) {
@@ -314,11 +357,11 @@ __global__ __launch_bounds__(256, NT == 8 ? 2 : 3) void product_kernel(LogitsArg
             const int64_t row = row0 + lane % L * W;
             if (row < a.V) {
                 float bias[W];
-                #pragma unroll
+#pragma unroll
                 for (int i = 0; i < W; ++i) bias[i] = a.bias ? a.bias[row + i] : 0.f;
-                for (int t = lane / L; t < 16 && b0 + t < a.B; t += 64 / L) {
+                for (int t = lane / L; t < G && b0 + t < a.B; t += 64 / L) {
                     float v[W];
-                    #pragma unroll
+#pragma unroll
                     for (int i = 0; i < W; ++i) v[i] = buf[t * OW + lane % L * W + i] + bias[i];
                     T* to = (T*)a.out + (b0 + t) * a.V + row;
                     if constexpr (sizeof(T) == 4) *(float4*)to = make_float4(v[0], v[1], v[2], v[3]);
@@ -330,7 +373,7 @@ __global__ __launch_bounds__(256, NT == 8 ? 2 : 3) void product_kernel(LogitsArg
             const int64_t row = row0 + lane % L;
             if (row < a.V) {
                 const float bias = a.bias ? a.bias[row] : 0.f;
-                for (int t = lane / L; t < 16 && b0 + t < a.B; t += 64 / L) {
+                for (int t = lane / L; t < G && b0 + t < a.B; t += 64 / L) {
                     const float v = buf[t * OW + lane % L] + bias;
                     T* to = (T*)a.out + (b0 + t) * a.V + row;
                     if constexpr (sizeof(T) == 4) *to = v;
@@ -338,7 +381,7 @@ __global__ __launch_bounds__(256, NT == 8 ? 2 : 3) void product_kernel(LogitsArg
                 }
             }
         }
-        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_wave_barrier();                          // the next group overwrites what this one reads
     }
 }
 
@@ -405,15 +448,14 @@ extern "C" int csv_mx4_head_create(const uint8_t* d_codes, const uint8_t* d_scal
     x->V = V;
     x->d = d;
     x->chunks = chunks_of(d);
-    const int64_t tiles = ((int64_t)V + HEAD_ROWS - 1) / HEAD_ROWS * (HEAD_ROWS / 16), pieces = tiles * x->chunks * 64;
+    const int64_t bands = ((int64_t)V + HEAD_ROWS - 1) / HEAD_ROWS * (HEAD_ROWS / 64), pieces = bands * x->chunks * 256;
     const hipStream_t st = (hipStream_t)stream;
     hipError_t e = hipGetDevice(&x->device);
-    if (e == hipSuccess) e = hipMalloc((void**)&x->codes, (size_t)pieces * 16);
-    if (e == hipSuccess) e = hipMalloc((void**)&x->scales, (size_t)tiles * ((x->chunks + 3) / 4) * 256);
+    if (e == hipSuccess) e = hipMalloc((void**)&x->bands, (size_t)(bands * band_bytes(x->chunks)));
     if (e == hipSuccess && d_b) e = hipMalloc((void**)&x->bias, (size_t)V * 4);
     if (e == hipSuccess && d_b) e = hipMemcpyAsync(x->bias, d_b, (size_t)V * 4, hipMemcpyDeviceToDevice, st);
     if (e == hipSuccess) {
-        lay_out_kernel<<<(unsigned)((pieces + 255) / 256), 256, 0, st>>>(d_codes, d_scales, V, d, x->chunks, pieces, x->codes, x->scales);
+        lay_out_kernel<<<(unsigned)((pieces + 255) / 256), 256, 0, st>>>(d_codes, d_scales, V, d, x->chunks, pieces, x->bands);
         e = hipGetLastError();
     }
     if (e == hipSuccess) e = hipStreamSynchronize(st);
@@ -435,7 +477,7 @@ extern "C" int csv_mx4_head_dims(const csv_mx4_head* x, int* V, int* d) {
 
 extern "C" void csv_mx4_head_free(csv_mx4_head* x) {
     if (!x) return;
-    void* ptrs[] = {x->codes, x->scales, x->bias};
+    void* ptrs[] = {x->bands, x->bias};
     for (void* p : ptrs)
         if (p) (void)hipFree(p);
     free(x);
@@ -447,10 +489,9 @@ static int check_logits(const csv_mx4_head* x, int B, int act) {
     if (act != CSV_ACT_BF16 && act != CSV_ACT_MX4) { csv_set_error("bad act=%d", act); return CSV_EINVAL; }
     return CSV_OK;
 }
-// groups of 16 hidden states that a block of the product takes together, and tiles of the 4-bit copy of h: whole blocks
-static inline int groups_of(int B) { return B <= 16 ? 1 : B <= 32 ? 2 : B <= 64 ? 4 : 8; }
+// tiles of the 4-bit copy of h: a whole number of what a block of the product takes together
 static inline int64_t tiles_of(int B) {
-    const int64_t nt = groups_of(B);
+    const int64_t nt = B <= 16 ? 1 : B <= 32 ? 2 : B <= 64 ? 4 : 8;
     return ((int64_t)B + 16 * nt - 1) / (16 * nt) * nt;
 }
 
@@ -479,7 +520,7 @@ extern "C" int csv_mx4_logits(const csv_mx4_head* x, const uint16_t* d_h, int B,
     if (dev != x->device) { csv_set_error("the head lives on device %d, the current device is %d", x->device, dev); return CSV_EINVAL; }
     const hipStream_t st = (hipStream_t)stream;
     LogitsArgs a = {};
-    a.codes = x->codes; a.scales = x->scales; a.bias = x->bias; a.V = x->V; a.d = x->d; a.chunks = x->chunks; a.B = B; a.h = d_h; a.out = d_logits;
+    a.bands = x->bands; a.bias = x->bias; a.V = x->V; a.d = x->d; a.chunks = x->chunks; a.B = B; a.h = d_h; a.out = d_logits;
     a.wide = ((uintptr_t)d_logits & 15) == 0 && x->V % (out_type == CSV_F32 ? 4 : 8) == 0;
     const int64_t tt = tiles_of(B);
     if (act == CSV_ACT_MX4) {
@@ -490,14 +531,22 @@ extern "C" int csv_mx4_logits(const csv_mx4_head* x, const uint16_t* d_h, int B,
         a.hc = hc;
         a.hs = (const uint32_t*)hs;
     }
-    switch (groups_of(B) * 2 + act) {
-        case 2: return launch_product<false, 1, 2, 4>(a, out_type, st);
-        case 3: return launch_product<true, 1, 2, 4>(a, out_type, st);
-        case 4: return launch_product<false, 2, 2, 2>(a, out_type, st);
-        case 5: return launch_product<true, 2, 2, 4>(a, out_type, st);
-        case 8: return launch_product<false, 4, 4, 1>(a, out_type, st);
-        case 9: return launch_product<true, 4, 4, 2>(a, out_type, st);
-        case 16: return launch_product<false, 8, 4, 1>(a, out_type, st);
-        default: return launch_product<true, 8, 4, 2>(a, out_type, st);
+    // Waves that take 64 rows each read h least often, waves of 32 rows make more blocks: below three blocks for two compute units
+    // the units that have none, or two, cost more.  Microseconds, 16 / 32 / 64 rows a wave:
+    // bf16, 14 hidden states, 80000 x 4096: 36.2 / 36.5 / 39.8, 16 of them, 128256 x 4096: 60.6 / 55.7 / 51.1;  30, 80000 x 4096: - / 40.6 / 43.9,
+    // 32, 256000 x 4608: - / 135 / 131;  4 bits, 64, 128256 x 8192: - / 119 / 113, 60, 80000 x 4096: - / 43.0 / 45.7.
+    const int64_t full = ((int64_t)x->V + 255) / 256;             // blocks of four waves of 64 rows
+    const int64_t fill = 384;
+    if (act == CSV_ACT_BF16) {
+        if (B <= 16) return full >= fill ? launch_product<false, 1, 4, 2>(a, out_type, st) : launch_product<false, 1, 2, 4>(a, out_type, st);
+        if (B <= 32) return full >= fill ? launch_product<false, 2, 4, 2>(a, out_type, st) : launch_product<false, 2, 2, 2>(a, out_type, st);
+        // where groups of 64 make too few blocks, groups of 32 read W more often, from cache: 60 hidden states, 50000 x 4096, 36.9 against
+        // 44.1; 400, 128256 x 4096, 392 against 367.  Groups of 128 win nothing: widening W is hidden behind the products already
+        return full * ((B + 63) / 64) >= fill ? launch_product<false, 4, 4, 1>(a, out_type, st) : launch_product<false, 2, 4, 2>(a, out_type, st);
     }
+    if (B <= 16) return full >= fill ? launch_product<true, 1, 4, 2>(a, out_type, st) : launch_product<true, 1, 2, 4>(a, out_type, st);
+    if (B <= 32) return launch_product<true, 2, 2, 4>(a, out_type, st);
+    if (B <= 64) return full >= fill ? launch_product<true, 4, 4, 1>(a, out_type, st) : launch_product<true, 4, 2, 2>(a, out_type, st);
+    // 100 hidden states: 24000 x 4096, 28.8 against 23.9 in groups of 64; 60000 x 2048, 22.7 against 26.8
+    return full * ((B + 127) / 128) >= fill / 2 ? launch_product<true, 8, 4, 2>(a, out_type, st) : launch_product<true, 4, 2, 2>(a, out_type, st);
 }

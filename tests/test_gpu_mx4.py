@@ -124,7 +124,8 @@ def test_logits_of_a_head(V, d, act, B):
 
 
 @pytest.mark.parametrize("act", [0, 1])
-@pytest.mark.parametrize("V,d,B", [(2000, 4096, 7), (777, 8192, 40), (513, 6152, 300), (20000, 264, 64), (40007, 136, 512)])
+@pytest.mark.parametrize("V,d,B", [(2000, 4096, 7), (777, 8192, 40), (513, 6152, 300), (20000, 264, 64), (40007, 136, 512),
+                                   (98305, 264, 9), (98307, 136, 30), (98400, 264, 61), (98320, 392, 70)])
 def test_logits_of_long_rows_and_many_rows(V, d, B, act):
     csv = _csv()
     log(f"logits V={V} d={d} act={act} B={B}")

@@ -7,6 +7,7 @@ without the built library raises.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from dataclasses import dataclass
 
@@ -389,58 +390,47 @@ def csv_full_logits(ws: CsvWorkspace, index: CsvIndex, h: torch.Tensor, out: tor
 
 _TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.int16: BF16}     # int16: bf16 patterns
 
-
-def _rows(t: torch.Tensor, what: str) -> int:
-    """The element type of a [rows, columns] tensor on the current device whose rows are contiguous."""
-    ty = _TYPES.get(t.dtype)
-    if ty is None or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{what} must be 2-D float32 or bfloat16 with contiguous rows")
-    _here(t, what)
-    return ty
+# The calls below are short next to a kernel of a few microseconds, so their checks are plain comparisons; the device and the raw stream
+# are asked for without building stream objects.
 
 
-def _ld(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
-
-
-def _here(t: torch.Tensor, what: str) -> None:
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+def _rows(t: torch.Tensor, what: str) -> tuple:
+    """(element type, device, elements from row to row) of a [rows, columns] tensor on the current device whose rows are contiguous."""
+    ty, dev = _TYPES.get(t.dtype), t.get_device()
+    if ty is None or t.dim() != 2:
+        raise ValueError(f"{what} must be 2-D, float32 or bfloat16")
+    rows, cols = t.shape
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError(f"{what} must have contiguous rows")
+    if dev < 0 or dev != torch._C._cuda_getDevice():
         raise ValueError(f"{what} must be on the current CUDA device")
+    return ty, dev, ld if rows > 1 else cols
 
 
-def _dense(t: torch.Tensor, what: str, dtype, *shape) -> int:
-    """Pointer of a contiguous tensor of this type and shape on the current device."""
-    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {shape}")
-    _here(t, what)
+def _dense(t: torch.Tensor, what: str, dtype, shape: tuple, dev: int) -> int:
+    """Pointer of a contiguous tensor of this type and shape on device `dev`."""
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {shape} on the device of the call")
     return t.data_ptr()
 
 
-class _On:
-    """What a call allocates belongs to the stream that the call runs on."""
-
-    def __init__(self, stream):
-        self._guard = None if stream is None else torch.cuda.stream(stream)
-
-    def __enter__(self):
-        if self._guard is not None:
-            self._guard.__enter__()
-
-    def __exit__(self, *exc):
-        if self._guard is not None:
-            self._guard.__exit__(*exc)
+def _device_of(t: torch.Tensor, what: str) -> int:
+    dev = t.get_device()
+    if dev < 0 or dev != torch._C._cuda_getDevice():
+        raise ValueError(f"{what} must be on the current CUDA device")
+    return dev
 
 
-def _scratch(need: int, scratch, device) -> tuple:
+def _scratch(need: int, scratch, dev: int) -> tuple:
     """(tensor that keeps the memory alive, pointer, bytes); the caller's scratch where it is given."""
     if scratch is not None:
-        _here(scratch, "scratch")
-        if not scratch.is_contiguous():
-            raise ValueError("scratch must be contiguous")
+        if scratch.get_device() != dev or not scratch.is_contiguous():
+            raise ValueError("scratch must be contiguous and on the device of the call")
         return scratch, scratch.data_ptr(), scratch.numel() * scratch.element_size()
     if need == 0:
         return None, None, 0
-    t = torch.empty(need, dtype=torch.uint8, device=device)
+    t = torch.empty(need, dtype=torch.uint8, device=dev)
     return t, t.data_ptr(), need
 
 
@@ -451,30 +441,34 @@ def mx4_padded(d: int) -> int:
 
 def csv_mx4_quantize(x: torch.Tensor, codes: torch.Tensor | None = None, scales: torch.Tensor | None = None, stream=None):
     """(codes uint8 [rows, dp/2], scales uint8 [rows, dp/32]) of the rows of x, bfloat16 or float32 [rows, d]."""
-    ty = _rows(x, "x")
+    if stream is not None:
+        with torch.cuda.stream(stream):         # what the call allocates belongs to the stream that it runs on
+            return csv_mx4_quantize(x, codes, scales)
+    ty, dev, ld = _rows(x, "x")
     rows, d = x.shape
     dp = mx4_padded(d)
-    with _On(stream):
-        if codes is None:
-            codes = torch.empty((rows, dp // 2), dtype=torch.uint8, device=x.device)
-        if scales is None:
-            scales = torch.empty((rows, dp // 32), dtype=torch.uint8, device=x.device)
-        _check(lib.csv_mx4_quantize(x.data_ptr(), ty, _ld(x), rows, d, _dense(codes, "codes", torch.uint8, rows, dp // 2),
-                                    _dense(scales, "scales", torch.uint8, rows, dp // 32), _stream(stream)))
+    if codes is None:
+        codes = torch.empty((rows, dp // 2), dtype=torch.uint8, device=dev)
+    if scales is None:
+        scales = torch.empty((rows, dp // 32), dtype=torch.uint8, device=dev)
+    _check(lib.csv_mx4_quantize(x.data_ptr(), ty, ld, rows, d, _dense(codes, "codes", torch.uint8, (rows, dp // 2), dev),
+                                _dense(scales, "scales", torch.uint8, (rows, dp // 32), dev), torch._C._cuda_getCurrentRawStream(dev)))
     return codes, scales
 
 
 def csv_mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, d: int, out: torch.Tensor | None = None, dtype=torch.bfloat16, stream=None):
     """The values [rows, d] that codes and scales stand for."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return csv_mx4_dequantize(codes, scales, d, out, dtype)
     rows, dp = codes.shape[0], mx4_padded(d)
-    with _On(stream):
-        if out is None:
-            out = torch.empty((rows, d), dtype=dtype, device=codes.device)
-        ty = _rows(out, "out")
-        if tuple(out.shape) != (rows, d):
-            raise ValueError(f"out must have the shape {(rows, d)}")
-        _check(lib.csv_mx4_dequantize(_dense(codes, "codes", torch.uint8, rows, dp // 2), _dense(scales, "scales", torch.uint8, rows, dp // 32),
-                                      rows, d, out.data_ptr(), ty, _ld(out), _stream(stream)))
+    if out is None:
+        out = torch.empty((rows, d), dtype=dtype, device=_device_of(codes, "codes"))
+    ty, dev, ld = _rows(out, "out")
+    if out.shape != (rows, d):
+        raise ValueError(f"out must have the shape {(rows, d)}")
+    _check(lib.csv_mx4_dequantize(_dense(codes, "codes", torch.uint8, (rows, dp // 2), dev), _dense(scales, "scales", torch.uint8, (rows, dp // 32), dev),
+                                  rows, d, out.data_ptr(), ty, ld, torch._C._cuda_getCurrentRawStream(dev)))
     return out
 
 
@@ -486,6 +480,12 @@ class CsvMx4Head:
         V, d = C.c_int(), C.c_int()
         _check(lib.csv_mx4_head_dims(self._h, C.byref(V), C.byref(d)))
         self.V, self.d = V.value, d.value
+
+    def scratch_bytes(self, B: int, act: int) -> int:
+        """Bytes of scratch that csv_mx4_logits needs for B hidden states."""
+        need = C.c_size_t()
+        _check(lib.csv_mx4_logits_scratch(self._h, B, act, C.byref(need)))
+        return need.value
 
     def free(self) -> None:
         if self._h:
@@ -501,72 +501,83 @@ class CsvMx4Head:
 
 def csv_mx4_head(codes: torch.Tensor, scales: torch.Tensor, b, d: int, stream=None) -> CsvMx4Head:
     """A head of 4-bit rows [V, d] (csv_mx4_quantize of W, or a checkpoint), laid out for csv_mx4_logits; b: float32 CUDA [V] or None."""
-    V, dp = codes.shape[0], mx4_padded(d)
+    V, dp, dev = codes.shape[0], mx4_padded(d), _device_of(codes, "codes")
     out = C.c_void_p()
-    _check(lib.csv_mx4_head_create(_dense(codes, "codes", torch.uint8, V, dp // 2), _dense(scales, "scales", torch.uint8, V, dp // 32),
-                                   None if b is None else _dense(b, "b", torch.float32, V), V, d, _stream(stream), C.byref(out)))
+    _check(lib.csv_mx4_head_create(_dense(codes, "codes", torch.uint8, (V, dp // 2), dev), _dense(scales, "scales", torch.uint8, (V, dp // 32), dev),
+                                   None if b is None else _dense(b, "b", torch.float32, (V,), dev), V, d, _stream(stream), C.byref(out)))
     return CsvMx4Head(out.value)
 
 
 def csv_mx4_logits(head: CsvMx4Head, h: torch.Tensor, out: torch.Tensor | None = None, act: int = ACT_BF16, dtype=torch.float32,
                    scratch: torch.Tensor | None = None, stream=None):
     """Logits [B, V] of hidden states h [B, d] (bf16 patterns) from a 4-bit head; act ACT_MX4 rounds h to 4 bits first."""
-    _dev2(h, "h")
-    _here(h, "h")
-    if h.dim() != 2 or h.shape[1] != head.d or h.dtype not in (torch.bfloat16, torch.int16):
-        raise ValueError(f"h must be [B, {head.d}] in bfloat16")
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return csv_mx4_logits(head, h, out, act, dtype, scratch)
+    dev = _device_of(h, "h")
+    if h.dim() != 2 or h.shape[1] != head.d or h.dtype not in (torch.bfloat16, torch.int16) or not h.is_contiguous():
+        raise ValueError(f"h must be a contiguous [B, {head.d}] tensor in bfloat16")
     B = h.shape[0]
-    with _On(stream):
-        if out is None:
-            out = torch.empty((B, head.V), dtype=dtype, device=h.device)
-        ty = _TYPES.get(out.dtype)
-        if ty is None:
-            raise ValueError("out must be float32 or bfloat16")
-        need = C.c_size_t()
-        _check(lib.csv_mx4_logits_scratch(head._h, B, act, C.byref(need)))
-        keep, ptr, size = _scratch(need.value, scratch, h.device)
-        _check(lib.csv_mx4_logits(head._h, h.data_ptr(), B, act, _dense(out, "out", out.dtype, B, head.V), ty, ptr, size, _stream(stream)))
+    if out is None:
+        out = torch.empty((B, head.V), dtype=dtype, device=dev)
+    ty = _TYPES.get(out.dtype)
+    if ty is None:
+        raise ValueError("out must be float32 or bfloat16")
+    keep, ptr, size = _scratch(0 if act == ACT_BF16 else head.scratch_bytes(B, act), scratch, dev)
+    _check(lib.csv_mx4_logits(head._h, h.data_ptr(), B, act, _dense(out, "out", out.dtype, (B, head.V), dev), ty, ptr, size,
+                              torch._C._cuda_getCurrentRawStream(dev)))
     return out
+
+
+@functools.lru_cache(maxsize=256)
+def csv_loss_scratch(N: int, V: int) -> int:
+    """Bytes of scratch that csv_token_logprobs and csv_policy_loss need for logits [N, V]."""
+    need = C.c_size_t()
+    _check(lib.csv_loss_scratch(N, V, C.byref(need)))
+    return need.value
 
 
 def csv_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, inv_temperature: float = 1.0, logp: torch.Tensor | None = None,
                        stats: torch.Tensor | None = None, scratch: torch.Tensor | None = None, stream=None):
     """(logp float32 [N], stats float32 [N, 2]) of tokens int32 [N] under logits [N, V], float32 or bfloat16."""
-    ty = _rows(logits, "logits")
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return csv_token_logprobs(logits, tokens, inv_temperature, logp, stats, scratch)
+    ty, dev, ld = _rows(logits, "logits")
     N, V = logits.shape
-    with _On(stream):
-        if logp is None:
-            logp = torch.empty(N, dtype=torch.float32, device=logits.device)
-        if stats is None:
-            stats = torch.empty((N, 2), dtype=torch.float32, device=logits.device)
-        need = C.c_size_t()
-        _check(lib.csv_loss_scratch(N, V, C.byref(need)))
-        keep, ptr, size = _scratch(need.value, scratch, logits.device)
-        _check(lib.csv_token_logprobs(logits.data_ptr(), ty, _ld(logits), N, V, _dense(tokens, "tokens", torch.int32, N), inv_temperature,
-                                      _dense(logp, "logp", torch.float32, N), _dense(stats, "stats", torch.float32, N, 2), ptr, size,
-                                      _stream(stream)))
+    if logp is None:
+        logp = torch.empty(N, dtype=torch.float32, device=dev)
+    if stats is None:
+        stats = torch.empty((N, 2), dtype=torch.float32, device=dev)
+    keep, ptr, size = _scratch(csv_loss_scratch(N, V), scratch, dev)
+    _check(lib.csv_token_logprobs(logits.data_ptr(), ty, ld, N, V, _dense(tokens, "tokens", torch.int32, (N,), dev), inv_temperature,
+                                  _dense(logp, "logp", torch.float32, (N,), dev), _dense(stats, "stats", torch.float32, (N, 2), dev), ptr, size,
+                                  torch._C._cuda_getCurrentRawStream(dev)))
     return logp, stats
 
 
-def _grad_of(logits: torch.Tensor, grad: torch.Tensor) -> tuple:
-    if _rows(grad, "grad") != _TYPES[logits.dtype] or grad.shape != logits.shape:
-        raise ValueError("grad must have the type and the shape of the logits")
-    return grad.data_ptr(), _ld(grad)
+def _grad_of(logits: torch.Tensor, grad: torch.Tensor, ty: int, dev: int) -> tuple:
+    gty, gdev, gld = _rows(grad, "grad")
+    if gty != ty or gdev != dev or grad.shape != logits.shape:
+        raise ValueError("grad must have the type, the shape and the device of the logits")
+    return grad.data_ptr(), gld
 
 
 def csv_token_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor, stats: torch.Tensor, grad_logp: torch.Tensor,
                                 inv_temperature: float = 1.0, grad: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """The gradient by the logits, [N, V] in their type, from the stats of csv_token_logprobs and the gradient by logp (float32 [N]).
     grad may be the logits themselves."""
-    ty = _rows(logits, "logits")
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return csv_token_logprobs_backward(logits, tokens, stats, grad_logp, inv_temperature, grad)
+    ty, dev, ld = _rows(logits, "logits")
     N, V = logits.shape
-    with _On(stream):
-        if grad is None:
-            grad = torch.empty((N, V), dtype=logits.dtype, device=logits.device)
-        gp, gld = _grad_of(logits, grad)
-        _check(lib.csv_token_logprobs_backward(logits.data_ptr(), ty, _ld(logits), N, V, _dense(tokens, "tokens", torch.int32, N),
-                                               _dense(stats, "stats", torch.float32, N, 2), _dense(grad_logp, "grad_logp", torch.float32, N),
-                                               inv_temperature, gp, gld, _stream(stream)))
+    if grad is None:
+        grad = torch.empty((N, V), dtype=logits.dtype, device=dev)
+    gp, gld = _grad_of(logits, grad, ty, dev)
+    _check(lib.csv_token_logprobs_backward(logits.data_ptr(), ty, ld, N, V, _dense(tokens, "tokens", torch.int32, (N,), dev),
+                                           _dense(stats, "stats", torch.float32, (N, 2), dev), _dense(grad_logp, "grad_logp", torch.float32, (N,), dev),
+                                           inv_temperature, gp, gld, torch._C._cuda_getCurrentRawStream(dev)))
     return grad
 
 
@@ -576,25 +587,26 @@ def csv_policy_loss(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.
                     scratch: torch.Tensor | None = None, stream=None):
     """(loss float32 scalar tensor, logp float32 [N], grad [N, V] in the type of the logits, or None without want_grad and grad) of the
     clipped policy loss; weights are mask and normaliser in one.  grad may be the logits themselves."""
-    ty = _rows(logits, "logits")
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return csv_policy_loss(logits, tokens, old_logp, ref_logp, advantages, weights, clip_low, clip_high, beta, inv_temperature, loss,
+                                   logp, grad, want_grad, scratch)
+    ty, dev, ld = _rows(logits, "logits")
     N, V = logits.shape
-    f32 = torch.float32
-    with _On(stream):
-        if loss is None:
-            loss = torch.empty((), dtype=f32, device=logits.device)
-        if logp is None:
-            logp = torch.empty(N, dtype=f32, device=logits.device)
-        if grad is None and want_grad:
-            grad = torch.empty((N, V), dtype=logits.dtype, device=logits.device)
-        gp, gld = (None, 0) if grad is None else _grad_of(logits, grad)
-        params = PolicyParams(clip_low, clip_high, beta, inv_temperature)
-        need = C.c_size_t()
-        _check(lib.csv_loss_scratch(N, V, C.byref(need)))
-        keep, ptr, size = _scratch(need.value, scratch, logits.device)
-        _check(lib.csv_policy_loss(logits.data_ptr(), ty, _ld(logits), N, V, _dense(tokens, "tokens", torch.int32, N),
-                                   _dense(old_logp, "old_logp", f32, N), None if ref_logp is None else _dense(ref_logp, "ref_logp", f32, N),
-                                   _dense(advantages, "advantages", f32, N), _dense(weights, "weights", f32, N), C.byref(params),
-                                   _dense(loss, "loss", f32), _dense(logp, "logp", f32, N), gp, gld, ptr, size, _stream(stream)))
+    f32, n = torch.float32, (N,)
+    if loss is None:
+        loss = torch.empty((), dtype=f32, device=dev)
+    if logp is None:
+        logp = torch.empty(N, dtype=f32, device=dev)
+    if grad is None and want_grad:
+        grad = torch.empty((N, V), dtype=logits.dtype, device=dev)
+    gp, gld = (None, 0) if grad is None else _grad_of(logits, grad, ty, dev)
+    keep, ptr, size = _scratch(csv_loss_scratch(N, V), scratch, dev)
+    _check(lib.csv_policy_loss(logits.data_ptr(), ty, ld, N, V, _dense(tokens, "tokens", torch.int32, n, dev), _dense(old_logp, "old_logp", f32, n, dev),
+                               None if ref_logp is None else _dense(ref_logp, "ref_logp", f32, n, dev), _dense(advantages, "advantages", f32, n, dev),
+                               _dense(weights, "weights", f32, n, dev), C.byref(PolicyParams(clip_low, clip_high, beta, inv_temperature)),
+                               _dense(loss, "loss", f32, (), dev), _dense(logp, "logp", f32, n, dev), gp, gld, ptr, size,
+                               torch._C._cuda_getCurrentRawStream(dev)))
     return loss, logp, grad
 
 

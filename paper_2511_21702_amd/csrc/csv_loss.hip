@@ -1,24 +1,35 @@
 // Log-probabilities of given tokens from rows of logits, their gradient, and the clipped policy loss with its gradient.
 //
-//   row_kernel    one block per row of logits: the largest logit m and s = sum exp(c (x - m)), the log-probability of the row's token, and
-//                 as the call asks the row's loss term and its gradient row
-//   grad_kernel   gradient rows from given m, s and coefficients
-//   sum_kernel    the loss: the rows' terms in float64, in one order
+//   row_kernel     one block per row: the largest logit m and s = sum exp(c (x - m)), the log-probability of the row's token, and for the
+//                  policy loss the row's term and its gradient row, from a second read while the row is still in a cache
+//   part_kernel    m and s of a part of a row, for few rows; then
+//   join_kernel    the log-probabilities from the parts, or
+//   policy_kernel  the policy loss from the parts: every block joins its row's parts and writes its part of the gradient, the block that
+//                  finishes last adds the loss up
+//   grad_kernel    gradient rows from given m, s and coefficients
+//   sum_kernel     the loss: the rows' terms in float64, in one order
 //
 // A row starts wherever its stride puts it: it is read as up to E - 1 single elements, 16-byte pieces of E elements, and up to
 // E - 1 single elements (E = 4 or 8); the single ones go to the first threads, one each.
+//
+// Exponentials.  With c2 = c log2(e), exp(c (x - m)) = 2^(x c2 - m c2): one fused multiply-add and one exponential per logit, which matters,
+// because at bfloat16's bytes per logit the instructions cost as much as the memory.  k = m c2 is rounded, by at most 2^-5 while it is
+// below NEAR; what is lost, d = fma(m, c2, -k), is known exactly and taken out of the sum, so that s is relative to m itself.  Rows whose
+// largest logit lies further out (and rows of minus infinities, NaNs and plus infinities) take a second pass that subtracts first.
 #include "csv_common.h"
 
 #include <math.h>
 
-#define THREADS 1024
 #define LOG2E 1.44269504089f
-#define LOWEST (-3.402823466e38f)   // start of a running maximum: exp(c (-inf - LOWEST)) is 0, not NaN
+#define LOWEST (-3.402823466e38f)
+#define NEAR 524288.f               // 2^19
+#define MAX_PARTS 64                // parts of a row: one per lane of the wave that joins them
+#define PART_MIN 2048               // logits of a part, at least
 
 struct RowArgs {
     const void* x;
     int64_t ld;
-    int N, V;
+    int N, V, parts;
     const int32_t* tokens;
     float c;                 // inverse temperature
     const float* old_logp;   // policy loss
@@ -30,31 +41,44 @@ struct RowArgs {
     const float* grad_logp;
     float* logp;
     float* stats;
-    double* terms;
+    double* terms;           // scratch: [N]
+    float2* part;            // [N * parts] (m, s) of a part of a row
+    float* xt;               // [N] the logit of the row's token
+    int* arrived;            // rows whose term is there
     void* grad;
     int64_t ld_grad;
 };
 
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 template <typename T> struct Vec;
 template <> struct Vec<float> {
     static constexpr int E = 4;
     float v[4];
-    __device__ __forceinline__ void load(const float* p) { const float4 u = *(const float4*)p; v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w; }
-    __device__ __forceinline__ void store(float* p) const { *(float4*)p = make_float4(v[0], v[1], v[2], v[3]); }
+    __device__ __forceinline__ void widen(const v4u& u) {
+        for (int j = 0; j < 4; ++j) v[j] = __uint_as_float(u[j]);
+    }
+    __device__ __forceinline__ void load(const float* p) { widen(*(const v4u*)p); }
+    __device__ __forceinline__ void load_last(const float* p) { widen(__builtin_nontemporal_load((const v4u*)p)); }
+    __device__ __forceinline__ void store(float* p) const {
+        __builtin_nontemporal_store(v4u{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}, (v4u*)p);
+    }
 };
 template <> struct Vec<uint16_t> {
     static constexpr int E = 8;
     float v[8];
-    __device__ __forceinline__ void load(const uint16_t* p) {
-        const uint4 u = *(const uint4*)p;
-        v[0] = bf16_lo(u.x); v[1] = bf16_hi(u.x); v[2] = bf16_lo(u.y); v[3] = bf16_hi(u.y);
-        v[4] = bf16_lo(u.z); v[5] = bf16_hi(u.z); v[6] = bf16_lo(u.w); v[7] = bf16_hi(u.w);
+    __device__ __forceinline__ void widen(const v4u& u) {
+        for (int j = 0; j < 4; ++j) {
+            v[2 * j] = bf16_lo(u[j]);
+            v[2 * j + 1] = bf16_hi(u[j]);
+        }
     }
+    __device__ __forceinline__ void load(const uint16_t* p) { widen(*(const v4u*)p); }
+    __device__ __forceinline__ void load_last(const uint16_t* p) { widen(__builtin_nontemporal_load((const v4u*)p)); }
     __device__ __forceinline__ void store(uint16_t* p) const {
-        uint32_t w[4];
+        v4u w;
         for (int j = 0; j < 4; ++j)
             w[j] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * j]) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * j + 1]) << 16;
-        *(uint4*)p = make_uint4(w[0], w[1], w[2], w[3]);
+        __builtin_nontemporal_store(w, (v4u*)p);
     }
 };
 __device__ __forceinline__ float get(const float* p) { return *p; }
@@ -78,32 +102,122 @@ template <typename T> struct Row {
     }
 };
 
-// exp(c (x - m)) as 2^((x - m) c log2(e)); the difference is taken first, so that far logits keep their digits
-__device__ __forceinline__ float exp_at(float x, float m, float c2) { return __builtin_amdgcn_exp2f((x - m) * c2); }
+// 2^((x - m) c2)
+__device__ __forceinline__ float exp_far(float x, float m, float c2) { return __builtin_amdgcn_exp2f((x - m) * c2); }
 
-// c g ([j = t] - p_j) over a row, eg = c g, k = c g / s
-template <typename T>
-__device__ __forceinline__ void write_grad(const Row<T>& row, T* out, int V, int token, float m, float c2, float eg, float k) {
-    constexpr int E = Vec<T>::E;
-    const int tid = threadIdx.x, one = row.single(tid);
-    if (one >= 0) put(out + one, (one == token ? eg : 0.f) - k * exp_at(get(row.p + one), m, c2));
-    const bool aligned = ((uintptr_t)(out + row.head) & 15) == 0;
-    for (int i = tid; i < row.pieces; i += THREADS) {
+struct Stat {
+    float m, s;
+};
+
+// m and s of the single elements and the pieces lo .. hi - 1 of a row, by the whole block.  A thread keeps its own maximum and its sum
+// relative to max(m c2, -NEAR): what is masked, by minus infinity or by a number far down, adds 0 wherever it stands.
+// red: >= 16 words of LDS
+template <int THREADS, typename T>
+__device__ __forceinline__ Stat fold(const Row<T>& row, int lo, int hi, bool singles, float c2, float* red) {
+    constexpr int E = Vec<T>::E, U = 4;
+    const int one = singles ? row.single(threadIdx.x) : -1;
+    float m = -INFINITY, k = -NEAR, s = 0.f;
+    if (one >= 0) {
+        const float x = get(row.p + one);
+        m = fmaxf(m, x);
+        k = fmaxf(m * c2, -NEAR);
+        s = __builtin_amdgcn_exp2f(fmaf(x, c2, -k));
+    }
+    const T* base = row.p + row.head;
+    auto take = [&](const auto& x, int n) {
+        float top = m;
+        for (int u = 0; u < n; ++u)
+            for (int j = 0; j < E; ++j) top = fmaxf(top, x[u].v[j]);
+        const float kn = fmaxf(top * c2, -NEAR);
+        float add = 0.f;
+        for (int u = 0; u < n; ++u)
+            for (int j = 0; j < E; ++j) add += __builtin_amdgcn_exp2f(fmaf(x[u].v[j], c2, -kn));
+        s = fmaf(s, __builtin_amdgcn_exp2f(k - kn), add);
+        m = top;
+        k = kn;
+    };
+    int i = lo + threadIdx.x;
+    for (; i + (U - 1) * THREADS < hi; i += U * THREADS) {
+        Vec<T> x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u].load(base + (int64_t)(i + u * THREADS) * E);
+        take(x, U);
+    }
+    for (; i < hi; i += THREADS) {
+        Vec<T> x[1];
+        x[0].load(base + (int64_t)i * E);
+        take(x, 1);
+    }
+    Stat r;
+    r.m = block_max(m, red);
+    const float mc = r.m * c2, K = fmaxf(mc, -NEAR);
+    r.s = block_sum(s * __builtin_amdgcn_exp2f(k - K), red);
+    if (r.s > 0.f && fabsf(mc) < NEAR) {
+        r.s *= __builtin_amdgcn_exp2f(-fmaf(r.m, c2, -K));
+        return r;
+    }
+    const float base_m = fmaxf(r.m, LOWEST);                    // minus infinity less itself would be NaN
+    s = one >= 0 ? exp_far(get(row.p + one), base_m, c2) : 0.f;
+    for (i = lo + threadIdx.x; i < hi; i += THREADS) {
         Vec<T> x;
-        const int e0 = row.head + i * E;
-        x.load(row.p + e0);
-        for (int j = 0; j < E; ++j) x.v[j] = (e0 + j == token ? eg : 0.f) - k * exp_at(x.v[j], m, c2);
-        if (aligned) x.store(out + e0);
+        x.load(base + (int64_t)i * E);
+        for (int j = 0; j < E; ++j) s += exp_far(x.v[j], base_m, c2);
+    }
+    r.s = block_sum(s, red);
+    return r;
+}
+
+// c g ([j = t] - p_j) over the single elements and the pieces lo .. hi - 1 of a row; eg = c g
+template <int THREADS, bool FAR, typename T>
+__device__ __forceinline__ void write_part(const Row<T>& row, T* out, int lo, int hi, bool singles, int token, float m, float c2, float eg, float f) {
+    constexpr int E = Vec<T>::E, U = 4;
+    const float k = m * c2;
+    auto value = [&](float x) { return -f * (FAR ? exp_far(x, m, c2) : __builtin_amdgcn_exp2f(fmaf(x, c2, -k))); };
+    const int one = singles ? row.single(threadIdx.x) : -1;
+    if (one >= 0) put(out + one, (one == token ? eg : 0.f) + value(get(row.p + one)));
+    const T* from = row.p + row.head;
+    T* to = out + row.head;
+    const bool aligned = ((uintptr_t)to & 15) == 0;
+    const int special = token >= row.head ? (token - row.head) / E : -1;      // the piece with the token
+    auto give = [&](Vec<T>& x, int i) {
+        for (int j = 0; j < E; ++j) x.v[j] = value(x.v[j]);
+        if (i == special)
+            for (int j = 0; j < E; ++j) x.v[j] += row.head + i * E + j == token ? eg : 0.f;
+        if (aligned) x.store(to + (int64_t)i * E);
         else
-            for (int j = 0; j < E; ++j) put(out + e0 + j, x.v[j]);
+            for (int j = 0; j < E; ++j) put(to + (int64_t)i * E + j, x.v[j]);
+    };
+    int i = lo + threadIdx.x;
+    for (; i + (U - 1) * THREADS < hi; i += U * THREADS) {
+        Vec<T> x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u].load_last(from + (int64_t)(i + u * THREADS) * E);
+#pragma unroll
+        for (int u = 0; u < U; ++u) give(x[u], i + u * THREADS);
+    }
+    for (; i < hi; i += THREADS) {
+        Vec<T> x;
+        x.load_last(from + (int64_t)i * E);
+        give(x, i);
     }
 }
-template <typename T>
-__device__ __forceinline__ void write_zeros(T* out, int V) {
+template <int THREADS, typename T>
+__device__ __forceinline__ void write_grad(const Row<T>& row, T* out, int lo, int hi, bool singles, int token, float m, float s, float c2, float eg) {
+    const float k = m * c2;
+    if (fabsf(k) < NEAR) write_part<THREADS, false>(row, out, lo, hi, singles, token, m, c2, eg, eg / s * __builtin_amdgcn_exp2f(-fmaf(m, c2, -k)));
+    else write_part<THREADS, true>(row, out, lo, hi, singles, token, m, c2, eg, eg / s);
+}
+template <int THREADS, typename T>
+__device__ __forceinline__ void write_zeros(T* out, int V, int part, int parts) {
     const Row<T> row(out, V);
-    const int one = row.single(threadIdx.x);
+    const int one = part == 0 ? row.single(threadIdx.x) : -1;
     if (one >= 0) put(out + one, 0.f);
-    for (int i = threadIdx.x; i < row.pieces; i += THREADS) *(uint4*)(out + row.head + i * Vec<T>::E) = make_uint4(0, 0, 0, 0);
+    const int hi = (int)((int64_t)row.pieces * (part + 1) / parts);
+    for (int i = (int)((int64_t)row.pieces * part / parts) + threadIdx.x; i < hi; i += THREADS) __builtin_nontemporal_store(v4u{0, 0, 0, 0}, (v4u*)(out + row.head + (int64_t)i * Vec<T>::E));
+}
+
+__device__ __forceinline__ double log_prob(Stat r, float xt, float c) {
+    return r.s == 0.f ? -INFINITY : (double)c * ((double)xt - (double)r.m) - log((double)r.s);
 }
 
 // The loss term of a row and its derivative by the log-probability, in float64: one thread per row does this, and close to a clip border
@@ -122,82 +236,154 @@ __device__ __forceinline__ double policy_term(const RowArgs& a, int i, double lo
     return w * term;
 }
 
+__device__ __forceinline__ bool left_out(const RowArgs& a, int i, int token, bool policy) {
+    return token < 0 || token >= a.V || (policy && a.weights[i] == 0.f);
+}
+
 template <typename T, bool POLICY>
-__global__ __launch_bounds__(THREADS) void row_kernel(RowArgs a) {
+__global__ __launch_bounds__(1024, 8) void row_kernel(RowArgs a) {
     __shared__ float red[16];
     __shared__ float coef;
-    constexpr int E = Vec<T>::E;
     const int i = blockIdx.x, tid = threadIdx.x, token = a.tokens[i];
     T* grad = POLICY && a.grad ? (T*)a.grad + (int64_t)i * a.ld_grad : nullptr;
-    if (token < 0 || token >= a.V || (POLICY && a.weights[i] == 0.f)) {
+    if (left_out(a, i, token, POLICY)) {
         if (tid == 0) {
             if (a.logp) a.logp[i] = 0.f;
             if (POLICY) a.terms[i] = 0.0;
             else a.stats[2 * i] = a.stats[2 * i + 1] = 0.f;
         }
-        if (grad) write_zeros(grad, a.V);
+        if (grad) write_zeros<1024>(grad, a.V, 0, 1);
         return;
     }
     const Row<T> row((const T*)a.x + (int64_t)i * a.ld, a.V);
-    const float c2 = a.c * LOG2E;
-    float m = LOWEST, s = 0.f;
-    const int one = row.single(tid);
-    if (one >= 0) {
-        const float x = get(row.p + one);
-        m = fmaxf(m, x);
-        s = exp_at(x, m, c2);
-    }
-    for (int k = tid; k < row.pieces; k += THREADS) {
-        Vec<T> x;
-        x.load(row.p + row.head + k * E);
-        float top = x.v[0];
-        for (int j = 1; j < E; ++j) top = fmaxf(top, x.v[j]);
-        top = fmaxf(m, top);
-        float add = 0.f;
-        for (int j = 0; j < E; ++j) add += exp_at(x.v[j], top, c2);
-        s = s * exp_at(m, top, c2) + add;
-        m = top;
-    }
-    const float M = block_max(m, red);
-    s = block_sum(s * exp_at(m, M, c2), red);
-    const float xt = get(row.p + token);
+    const float c2 = a.c * LOG2E, xt = get(row.p + token);
+    const Stat r = fold<1024>(row, 0, row.pieces, true, c2, red);
     if (tid == 0) {
-        const double logp = s == 0.f ? -INFINITY : (double)a.c * ((double)xt - (double)M) - log((double)s);
+        const double logp = log_prob(r, xt, a.c);
         if (a.logp) a.logp[i] = (float)logp;
         if (POLICY) {
             double g;
             a.terms[i] = policy_term(a, i, logp, g);
             coef = (float)(g * (double)a.c);
         } else {
-            a.stats[2 * i] = M;
-            a.stats[2 * i + 1] = s;
+            a.stats[2 * i] = r.m;
+            a.stats[2 * i + 1] = r.s;
         }
     }
     if (!POLICY || !grad) return;
     __syncthreads();                            // the row's token has been read by now: the gradient may replace the logits
-    if (s == 0.f) write_zeros(grad, a.V);
-    else write_grad(row, grad, a.V, token, M, c2, coef, coef / s);
+    if (r.s == 0.f) write_zeros<1024>(grad, a.V, 0, 1);
+    else write_grad<1024>(row, grad, 0, row.pieces, true, token, r.m, r.s, c2, coef);
+}
+
+template <typename T, bool POLICY>
+__global__ __launch_bounds__(256, 8) void part_kernel(RowArgs a) {
+    __shared__ float red[16];
+    const int i = blockIdx.x / a.parts, p = blockIdx.x % a.parts, token = a.tokens[i];
+    if (POLICY && blockIdx.x == 0 && threadIdx.x == 0) *a.arrived = 0;
+    if (left_out(a, i, token, POLICY)) return;
+    const Row<T> row((const T*)a.x + (int64_t)i * a.ld, a.V);
+    const Stat r = fold<256>(row, (int)((int64_t)row.pieces * p / a.parts), (int)((int64_t)row.pieces * (p + 1) / a.parts), p == 0, a.c * LOG2E, red);
+    if (threadIdx.x == 0) {
+        a.part[(int64_t)i * a.parts + p] = make_float2(r.m, r.s);
+        if (p == 0) a.xt[i] = get(row.p + token);
+    }
+}
+
+// m and s of row i from its parts, by a whole wave
+__device__ __forceinline__ Stat join(const RowArgs& a, int i) {
+    const int lane = threadIdx.x & 63;
+    float2 v = make_float2(-INFINITY, 0.f);
+    if (lane < a.parts) v = a.part[(int64_t)i * a.parts + lane];
+    Stat r;
+    r.m = wave_max(v.x);
+    r.s = wave_sum(v.y == 0.f ? 0.f : v.y * exp_far(v.x, r.m, a.c * LOG2E));
+    return r;
+}
+
+__global__ __launch_bounds__(256) void join_kernel(RowArgs a) {
+    const int i = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (i >= a.N) return;
+    Stat r = {0.f, 0.f};
+    float logp = 0.f;
+    if (!left_out(a, i, a.tokens[i], false)) {
+        r = join(a, i);
+        logp = (float)log_prob(r, a.xt[i], a.c);
+    }
+    if ((threadIdx.x & 63) == 0) {
+        a.logp[i] = logp;
+        a.stats[2 * i] = r.m;
+        a.stats[2 * i + 1] = r.s;
+    }
+}
+
+// The sum of the rows' terms, every thread in steps of the block, then a tree: one order for a given N.
+template <int THREADS>
+__device__ __forceinline__ double sum_terms(const double* terms, int N, double* part) {
+    double s = 0.0;
+    for (int i = threadIdx.x; i < N; i += THREADS)
+        s += __builtin_bit_cast(double, __hip_atomic_load((const unsigned long long*)terms + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+    for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = 0.0;
+    for (int w = 0; w < THREADS / 64; ++w) s += part[w];
+    return s;
 }
 
 template <typename T>
-__global__ __launch_bounds__(THREADS) void grad_kernel(RowArgs a) {
-    const int i = blockIdx.x, token = a.tokens[i];
-    T* grad = (T*)a.grad + (int64_t)i * a.ld_grad;
-    const float m = a.stats_in[2 * i], s = a.stats_in[2 * i + 1], g = a.grad_logp[i] * a.c;
-    if (token < 0 || token >= a.V || g == 0.f || s == 0.f) write_zeros(grad, a.V);
-    else write_grad(Row<T>((const T*)a.x + (int64_t)i * a.ld, a.V), grad, a.V, token, m, a.c * LOG2E, g, g / s);
+__global__ __launch_bounds__(256) void policy_kernel(RowArgs a, int parts, float* loss) {
+    __shared__ float coef;
+    __shared__ int last;
+    __shared__ double sums[4];
+    const int i = blockIdx.x / parts, p = blockIdx.x % parts, token = a.tokens[i];
+    T* grad = a.grad ? (T*)a.grad + (int64_t)i * a.ld_grad : nullptr;
+    const bool out = left_out(a, i, token, true);
+    Stat r = {0.f, 0.f};
+    if (!out) r = join(a, i);
+    if (threadIdx.x == 0) {
+        double logp = 0.0, g = 0.0, term = 0.0;
+        if (!out) {
+            logp = log_prob(r, a.xt[i], a.c);
+            term = policy_term(a, i, logp, g);
+        }
+        coef = (float)(g * (double)a.c);
+        last = 0;
+        if (p == 0) {
+            if (a.logp) a.logp[i] = (float)logp;
+            // The term goes out as an atomic store, past this die's cache, and has arrived before it is counted; a fence would write all of the
+            // cache's gradient rows back first (64 rows of 128256: 23 us against 10).
+            __hip_atomic_store((unsigned long long*)a.terms + i, __builtin_bit_cast(unsigned long long, term), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            last = __hip_atomic_fetch_add(a.arrived, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.N - 1;
+        }
+    }
+    __syncthreads();
+    if (grad) {
+        const Row<T> row((const T*)a.x + (int64_t)i * a.ld, a.V);
+        if (out || r.s == 0.f) write_zeros<256>(grad, a.V, p, parts);
+        else write_grad<256>(row, grad, (int)((int64_t)row.pieces * p / parts), (int)((int64_t)row.pieces * (p + 1) / parts), p == 0, token, r.m, r.s, a.c * LOG2E, coef);
+    }
+    if (last) {
+        const double s = sum_terms<256>(a.terms, a.N, sums);
+        if (threadIdx.x == 0) *loss = (float)s;
+    }
 }
 
-__global__ __launch_bounds__(THREADS) void sum_kernel(const double* __restrict__ terms, int N, float* __restrict__ loss) {
-    __shared__ double part[THREADS];
-    double s = 0.0;
-    for (int i = threadIdx.x; i < N; i += THREADS) s += terms[i];
-    part[threadIdx.x] = s;
-    for (int h = THREADS / 2; h > 0; h >>= 1) {
-        __syncthreads();
-        if (threadIdx.x < h) part[threadIdx.x] += part[threadIdx.x + h];
-    }
-    if (threadIdx.x == 0) *loss = (float)part[0];
+template <typename T>
+__global__ __launch_bounds__(256) void grad_kernel(RowArgs a) {
+    const int i = blockIdx.x / a.parts, p = blockIdx.x % a.parts, token = a.tokens[i];
+    T* grad = (T*)a.grad + (int64_t)i * a.ld_grad;
+    const float m = a.stats_in[2 * i], s = a.stats_in[2 * i + 1], g = a.grad_logp[i] * a.c;
+    const Row<T> row((const T*)a.x + (int64_t)i * a.ld, a.V);
+    if (left_out(a, i, token, false) || g == 0.f || s == 0.f) write_zeros<256>(grad, a.V, p, a.parts);
+    else write_grad<256>(row, grad, (int)((int64_t)row.pieces * p / a.parts), (int)((int64_t)row.pieces * (p + 1) / a.parts), p == 0, token, m, s, a.c * LOG2E, g);
+}
+
+__global__ __launch_bounds__(1024) void sum_kernel(const double* __restrict__ terms, int N, float* __restrict__ loss) {
+    __shared__ double part[16];
+    const double s = sum_terms<1024>(terms, N, part);
+    if (threadIdx.x == 0) *loss = (float)s;
 }
 
 // ------------------------------------------------------------------------------------------------ entry points
@@ -225,11 +411,35 @@ static int check_scratch(int N, int V, const void* p, size_t have) {
     return CSV_OK;
 }
 
+// Where the rows alone leave compute units without work, or with too little of it to keep the memory busy, a row is cut into parts.  Below
+// FEW_ROWS two launches over parts win, though they read the logits twice, from FEW_ROWS on one block per row does (policy loss, us,
+// parts / row: 64 rows of 128256 bf16 14.5 / 25, 250 of them 41 / 32, 1000 rows of 100000 float32 213 / 182).  Without a gradient one block
+// per row stays ahead up to LONG_ROW logits, where the second launch costs more than the parts save.
+#define FEW_ROWS 192
+#define LONG_ROW 65536
+#define PART_BLOCKS 2048            // blocks of 256 threads that are resident together
+#define GRAD_BLOCKS 16384           // gradients from given statistics have nothing to join: short blocks (us for 509 x 151669 bf16, 2048 x
+                                    // 128256 float32: 64, 412 with 4096 blocks, 54, 391 with 16384)
+static inline int parts_of(int N, int V, int most) {
+    const int by_rows = most / (N > 0 ? N : 1), by_length = (V + PART_MIN - 1) / PART_MIN;
+    const int p = by_rows < by_length ? by_rows : by_length;
+    return p < 1 ? 1 : p > MAX_PARTS ? MAX_PARTS : p;
+}
+
 extern "C" int csv_loss_scratch(int N, int V, size_t* bytes) {
     if (N < 0 || V < 1) { csv_set_error("need N >= 0 and V >= 1 (N=%d, V=%d)", N, V); return CSV_ESHAPE; }
     if (!bytes) { csv_set_error("null bytes"); return CSV_EINVAL; }
-    *bytes = (size_t)N * sizeof(double);
+    *bytes = (size_t)N * sizeof(double) + (N > 0 && N < FEW_ROWS ? (size_t)N * (sizeof(float2) * parts_of(N, V, PART_BLOCKS) + 8) + 8 : 0);
     return CSV_OK;
+}
+
+static void place_scratch(RowArgs& a, void* p) {
+    a.terms = (double*)p;
+    if (a.N >= FEW_ROWS) return;
+    a.parts = parts_of(a.N, a.V, PART_BLOCKS);
+    a.part = (float2*)(a.terms + a.N);
+    a.xt = (float*)(a.part + (size_t)a.N * a.parts);
+    a.arrived = (int*)(a.xt + 2 * (size_t)a.N);
 }
 
 extern "C" int csv_token_logprobs(const void* d_logits, int type, int64_t ld, int N, int V, const int32_t* d_tokens, float inv_temperature, float* d_logp,
@@ -240,8 +450,18 @@ extern "C" int csv_token_logprobs(const void* d_logits, int type, int64_t ld, in
     if (!d_logp || !d_stats) { csv_set_error("null d_logp or d_stats"); return CSV_EINVAL; }
     RowArgs a = {};
     a.x = d_logits; a.ld = ld; a.N = N; a.V = V; a.tokens = d_tokens; a.c = inv_temperature; a.logp = d_logp; a.stats = d_stats;
-    if (type == CSV_F32) row_kernel<float, false><<<N, THREADS, 0, (hipStream_t)stream>>>(a);
-    else row_kernel<uint16_t, false><<<N, THREADS, 0, (hipStream_t)stream>>>(a);
+    const hipStream_t st = (hipStream_t)stream;
+    if (N < FEW_ROWS && V > LONG_ROW) {
+        place_scratch(a, d_scratch);
+        if (type == CSV_F32) part_kernel<float, false><<<N * a.parts, 256, 0, st>>>(a);
+        else part_kernel<uint16_t, false><<<N * a.parts, 256, 0, st>>>(a);
+        CSV_LAUNCH_CHECK("part_kernel");
+        join_kernel<<<(N + 3) / 4, 256, 0, st>>>(a);
+        CSV_LAUNCH_CHECK("join_kernel");
+        return CSV_OK;
+    }
+    if (type == CSV_F32) row_kernel<float, false><<<N, 1024, 0, st>>>(a);
+    else row_kernel<uint16_t, false><<<N, 1024, 0, st>>>(a);
     CSV_LAUNCH_CHECK("row_kernel");
     return CSV_OK;
 }
@@ -255,8 +475,11 @@ extern "C" int csv_token_logprobs_backward(const void* d_logits, int type, int64
     RowArgs a = {};
     a.x = d_logits; a.ld = ld; a.N = N; a.V = V; a.tokens = d_tokens; a.c = inv_temperature; a.stats_in = d_stats; a.grad_logp = d_grad_logp;
     a.grad = d_grad; a.ld_grad = ld_grad;
-    if (type == CSV_F32) grad_kernel<float><<<N, THREADS, 0, (hipStream_t)stream>>>(a);
-    else grad_kernel<uint16_t><<<N, THREADS, 0, (hipStream_t)stream>>>(a);
+    a.parts = parts_of(N, V, GRAD_BLOCKS);
+    const int64_t n = (int64_t)N * a.parts;
+    if (n > 0x7fffffff) { csv_set_error("N=%d rows are too many blocks", N); return CSV_ESHAPE; }
+    if (type == CSV_F32) grad_kernel<float><<<(unsigned)n, 256, 0, (hipStream_t)stream>>>(a);
+    else grad_kernel<uint16_t><<<(unsigned)n, 256, 0, (hipStream_t)stream>>>(a);
     CSV_LAUNCH_CHECK("grad_kernel");
     return CSV_OK;
 }
@@ -277,14 +500,25 @@ extern "C" int csv_policy_loss(const void* d_logits, int type, int64_t ld, int N
     a.x = d_logits; a.ld = ld; a.N = N; a.V = V; a.tokens = d_tokens; a.c = p->inv_temperature;
     a.old_logp = d_old_logp; a.ref_logp = d_ref_logp; a.adv = d_advantages; a.weights = d_weights;
     a.clip_low = p->clip_low; a.clip_high = p->clip_high; a.beta = p->beta;
-    a.logp = d_logp; a.terms = (double*)d_scratch; a.grad = d_grad; a.ld_grad = ld_grad;
+    a.logp = d_logp; a.grad = d_grad; a.ld_grad = ld_grad;
+    place_scratch(a, d_scratch);
     const hipStream_t st = (hipStream_t)stream;
+    if (N > 0 && N < FEW_ROWS) {
+        if (type == CSV_F32) part_kernel<float, true><<<N * a.parts, 256, 0, st>>>(a);
+        else part_kernel<uint16_t, true><<<N * a.parts, 256, 0, st>>>(a);
+        CSV_LAUNCH_CHECK("part_kernel");
+        const int parts = d_grad ? a.parts : 1;
+        if (type == CSV_F32) policy_kernel<float><<<N * parts, 256, 0, st>>>(a, parts, d_loss);
+        else policy_kernel<uint16_t><<<N * parts, 256, 0, st>>>(a, parts, d_loss);
+        CSV_LAUNCH_CHECK("policy_kernel");
+        return CSV_OK;
+    }
     if (N > 0) {
-        if (type == CSV_F32) row_kernel<float, true><<<N, THREADS, 0, st>>>(a);
-        else row_kernel<uint16_t, true><<<N, THREADS, 0, st>>>(a);
+        if (type == CSV_F32) row_kernel<float, true><<<N, 1024, 0, st>>>(a);
+        else row_kernel<uint16_t, true><<<N, 1024, 0, st>>>(a);
         CSV_LAUNCH_CHECK("row_kernel");
     }
-    sum_kernel<<<1, THREADS, 0, st>>>(a.terms, N, d_loss);
+    sum_kernel<<<1, 1024, 0, st>>>(a.terms, N, d_loss);
     CSV_LAUNCH_CHECK("sum_kernel");
     return CSV_OK;
 }

@@ -35,13 +35,15 @@ def _place(x, dtype, gap=0, shift=0, fill=float("nan")):
     return v
 
 
-def _grad_close(got, p, s, t, g, c, rel, x, m, dtype):
+def _grad_close(got, p, s, t, g, c, rel, x, m, dtype, relg=None):
     """got against c g ([j = t] - p).  A probability carries the sum's error `rel` and, as in it, 4 U24 of its argument and one unit of the
-    exponential; coefficient, quotient, product and difference are rounded to float32 (4 U24 of what they make), the result to its type."""
+    exponential; coefficient, quotient, product and difference are rounded to float32 (4 U24 of what they make), the result to its type.
+    relg: what the coefficient itself is off by, relative."""
     want = O.grad_rows(p, s, t, g, c)
     a = np.abs(c * (np.where(np.isfinite(x), x, m[:, None]) - m[:, None]))
     cg = np.abs(c * g)[:, None]
     tol = cg * p * (rel[:, None] + (4 * a + 8) * O.U24) + (np.abs(want) + cg * (p > 0.5)) * 4 * O.U24
+    tol = tol + (np.abs(want) * relg[:, None] if relg is not None else 0.0)
     tol = tol * (1 + HALF[dtype]) + HALF[dtype] * np.abs(want) + TINY[dtype] * (1 + cg)
     with np.errstate(invalid="ignore"):
         ok = (np.abs(got - want) <= tol) | (np.isnan(got) & np.isnan(want))
@@ -217,10 +219,15 @@ def test_rows_beyond_32_bits(dtype):
     w = torch.zeros(N, device="cuda")
     w[rows] = torch.tensor([0.5, -0.25, 1.0], device="cuda")
     one = torch.ones(N, device="cuda")
-    want = csv.csv_policy_loss(small, ts, -one[:3], None, one[:3], w[rows])
-    loss, logp, grad = csv.csv_policy_loss(x, t, -one, None, one, w, grad=x)
-    assert torch.equal(logp[rows], want[1]) and torch.equal(grad[rows], want[2])
-    assert abs(float(loss) - float(want[0])) <= 2 * O.U24 * abs(float(want[0]))
+    x64, t64, w64 = small.cpu().double().numpy(), ts.cpu().numpy(), w[rows].cpu().double().numpy()
+    m, s, lp, p = O.rows_logp(x64, t64, 1.0)
+    tol, rel = O.logp_tolerance(x64, m, p, 1.0, lp)
+    # a clip of 1 and plus infinity: the loss is -w r A, its derivative -w A r, and both carry rel of the log-probability
+    loss, logp, grad = csv.csv_policy_loss(x, t, -one, None, one, w, clip_low=1.0, clip_high=float("inf"), grad=x)
+    assert (np.abs(logp[rows].cpu().double().numpy() - lp) <= tol).all()
+    term, g = O.policy(lp, -np.ones(3), None, np.ones(3), w64, 1.0, np.inf, 0.0)
+    assert abs(float(loss) - term.sum()) <= (np.abs(term) * rel).sum() * 1.01 + abs(term.sum()) * O.U24
+    _grad_close(grad[rows].cpu().double().numpy(), p, s, t64, g, 1.0, 2.01 * rel, x64, m, dtype, relg=1.01 * rel)
     assert not bool(grad[1:N - 2].any())
 
 

@@ -335,8 +335,9 @@ int csv_mx4_dequantize(const uint8_t* d_codes, const uint8_t* d_scales, int rows
  * A head of 4-bit microscaled rows: V rows of d elements in the format above (csv_mx4_quantize of W, or a checkpoint), laid
  * out once for the matrix cores (what the padding of a row holds does not matter).  d_b DEVICE float32[V] or NULL.  The head keeps copies of its own (about V*d*0.53 bytes): the
  * caller may free codes, scales and bias afterwards.  csv_mx4_head_create synchronises the stream before returning; on
- * error *out is NULL.
+ * error *out is NULL.  d <= CSV_MX4_MAX_D.
  */
+#define CSV_MX4_MAX_D (1 << 20)
 typedef struct csv_mx4_head csv_mx4_head;
 int csv_mx4_head_create(const uint8_t* d_codes, const uint8_t* d_scales, const float* d_b, int V, int d, void* stream,
                         csv_mx4_head** out);

@@ -3,7 +3,7 @@
 //   quantize_kernel     blocks of 32 elements -> one scale byte and 32 four-bit codes, row-major or in matrix-core tiles
 //   dequantize_kernel   the values that row-major codes stand for
 //   lay_out_kernel      row-major codes of a head -> tiles
-//   product_kernel      out[b, i] = <W_i, h_b> + b_i on the matrix cores
+//   product_kernel, many_kernel   out[b, i] = <W_i, h_b> + b_i on the matrix cores
 //
 // A tile is 16 rows x 128 elements: lane l of a wave holds the 32 elements of block l / 16 of row l % 16 (16 bytes) and that
 // block's scale, which is how v_mfma_scale_f32_16x16x128_f8f6f4 takes an operand.  Codes of a tile are 1 KB in lane order; the
@@ -14,6 +14,7 @@
 #include "csv_common.h"
 
 #include <stdlib.h>
+#include <type_traits>
 
 #define BLK 32        // elements of a block
 #define CHUNK 128     // elements of a row in a tile; rows are padded to a multiple of it
@@ -177,6 +178,46 @@ __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// The logits of G hidden states from b0 on and RT * 16 rows from row0 on, from a wave's part of LDS, where a hidden state is a row: so
+// that a row of logits is written in one piece per wave.
+template <int G, int RT, typename T>
+__device__ __forceinline__ void give_out(const LogitsArgs& a, const float* buf, int64_t b0, int64_t row0) {
+    constexpr int OW = RT * 16 + 4;
+    const int lane = threadIdx.x & 63;
+    __builtin_amdgcn_wave_barrier();
+    constexpr int W = sizeof(T) == 4 ? 4 : 8;                 // logits in 16 bytes
+    if (a.wide) {
+        constexpr int L = RT * 16 / W;                        // lanes of a hidden state
+        const int64_t row = row0 + lane % L * W;
+        if (row < a.V) {
+            float bias[W];
+#pragma unroll
+            for (int i = 0; i < W; ++i) bias[i] = a.bias ? a.bias[row + i] : 0.f;
+            for (int t = lane / L; t < G && b0 + t < a.B; t += 64 / L) {
+                float v[W];
+#pragma unroll
+                for (int i = 0; i < W; ++i) v[i] = buf[t * OW + lane % L * W + i] + bias[i];
+                T* to = (T*)a.out + (b0 + t) * a.V + row;
+                if constexpr (sizeof(T) == 4) *(float4*)to = make_float4(v[0], v[1], v[2], v[3]);
+                else *(v4u*)to = v4u{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+            }
+        }
+    } else {
+        constexpr int L = RT * 16;
+        const int64_t row = row0 + lane % L;
+        if (row < a.V) {
+            const float bias = a.bias ? a.bias[row] : 0.f;
+            for (int t = lane / L; t < G && b0 + t < a.B; t += 64 / L) {
+                const float v = buf[t * OW + lane % L] + bias;
+                T* to = (T*)a.out + (b0 + t) * a.V + row;
+                if constexpr (sizeof(T) == 4) *to = v;
+                else *to = __builtin_bit_cast(uint16_t, (__bf16)v);
+            }
+        }
+    }
+    __builtin_amdgcn_wave_barrier();                              // the next group overwrites what this one reads
+}
+
 // Four waves, RT tiles of 16 rows each, against NT groups of 16 hidden states; K goes by in stages of S tiles of 128.
 //
 // The sum over k may run in any order that both operands share.  A tile puts element 32 (l / 16) + 8 s + j at lane l, so a 4-bit tile goes to
@@ -185,18 +226,12 @@ __device__ __forceinline__ void lds_barrier() {
 // stage of h lies in LDS, two buffers, and passes through registers on its way there, so that a barrier waits for no load.  bf16 h lies row by
 // row with the 16-byte pieces of row t exchanged by t % 16 (a column of pieces then spreads over all banks); 4-bit h lies as its tiles.
 // Past the end of a row or of the batch the last piece or row is read again: codes of W are 0 there, and those hidden states are not stored.
-// With many hidden states in four bits the product is bound by the matrix cores, and 32x32x64 instructions run at 1.7 times the rate of
-// 16x16x128 (6.6 and 3.85 PFLOP/s measured on registers alone).  Lane l of theirs holds a block of row l % 32: two tiles side by side, read
-// in pieces of 256 bytes, blocks l / 32 and then 2 + l / 32 of a step.
 template <bool MX4, int NT, int RT, int S, typename T>
-__global__ __launch_bounds__(256, NT == 8 ? 2 : 3) void product_kernel(LogitsArgs a) {
+__global__ __launch_bounds__(256, 3) void product_kernel(LogitsArgs a) {
     constexpr int HP = NT * S * (MX4 ? 64 : 256);                 // 16-byte pieces of a stage of h
     constexpr int HT = (HP + 255) / 256;                          // of them per thread
-    constexpr bool BIG = MX4 && NT == 8;                          // 32x32x64 instructions
-    constexpr int G = BIG ? 32 : 16;                              // hidden states of an instruction
     constexpr int OW = RT * 16 + 4;                               // floats per hidden state in a wave's part of the output buffer
-    constexpr int LDS = 2 * HP > 4 * G * OW / 4 ? 2 * HP : 4 * G * OW / 4;
-    static_assert(!BIG || RT == 4, "a wave takes whole bands");
+    constexpr int LDS = 2 * HP > 16 * OW ? 2 * HP : 16 * OW;      // four waves' parts
     __shared__ v4u lds[LDS];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, col = lane & 15;
     // blocks of one die (every eighth) take the groups of hidden states of one block of rows after each other: W comes from that die's cache
@@ -205,30 +240,24 @@ __global__ __launch_bounds__(256, NT == 8 ? 2 : 3) void product_kernel(LogitsArg
     const int chunks = a.chunks, quads = (chunks + 3) >> 2, stages = (chunks + S - 1) / S;
     const int64_t tile0 = (int64_t)block * (4 * RT) + wave * RT;
     const uint8_t* band = a.bands + (tile0 >> 2) * band_bytes(chunks);
-    // where in a run of 64-lane tiles this lane's block is, in lanes; registers r of a step are r tiles on, or (BIG) tiles 2 (r / 2), blocks 2 (r % 2)
-    const int at = BIG ? (lane >> 4 & 1) * 64 + (lane >> 5) * 16 + col : lane;
-    auto step = [](int r) { return BIG ? (r >> 1) * 128 + (r & 1) * 32 : r * 64; };
-    const uint8_t *wc = band + (tile0 & 3) * 1024 + at * 16, *ws = band + (tile0 & 3) * 256 + at * 4;
+    const uint8_t *wc = band + (tile0 & 3) * 1024 + lane * 16, *ws = band + (tile0 & 3) * 256 + lane * 4;
     const int64_t htile0 = (int64_t)group * NT;
-    const uint32_t* hs = MX4 ? a.hs + htile0 * quads * 64 : nullptr;
+    const uint32_t* hs = MX4 ? a.hs + htile0 * quads * 64 + lane : nullptr;
 
     v4u w[S][RT], hr[HT];
     uint32_t sw[RT], sh[MX4 ? NT : 1], sw_next[RT], sh_next[MX4 ? NT : 1];
     auto load_w = [&](int c, v4u (&to)[RT]) {
         const int cc = min(c, chunks - 1);
 #pragma unroll
-        for (int r = 0; r < RT; ++r) to[r] = *(const v4u*)(wc + codes_at(cc) + step(r) * 16);
+        for (int r = 0; r < RT; ++r) to[r] = *(const v4u*)(wc + codes_at(cc) + r * 1024);
     };
     auto load_scales = [&](int c0) {                              // a stage lies within four tiles
         const int q = min(c0, chunks - 1) >> 2;
 #pragma unroll
-        for (int r = 0; r < RT; ++r) sw_next[r] = *(const uint32_t*)(ws + scales_at(q) + step(r) * 4);
+        for (int r = 0; r < RT; ++r) sw_next[r] = *(const uint32_t*)(ws + scales_at(q) + r * 256);
         if (MX4)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const int i = at + step(n);                      // tile i / 64
-                sh_next[n] = hs[((int64_t)(i >> 6) * quads + q) * 64 + (i & 63)];
-            }
+            for (int n = 0; n < NT; ++n) sh_next[n] = hs[((int64_t)n * quads + q) * 64];
     };
     auto load_h = [&](int c0) {
 #pragma unroll
@@ -253,29 +282,14 @@ __global__ __launch_bounds__(256, NT == 8 ? 2 : 3) void product_kernel(LogitsArg
             lds[buf * HP + (MX4 ? p : p ^ (p >> 4 & 15))] = hr[i];
         }
     };
-    v16f big[BIG ? 2 : 1][BIG ? 4 : 1];
+    v4f acc[RT][NT];
 #pragma unroll
-    for (int r = 0; r < (BIG ? 2 : 1); ++r)
+    for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int n = 0; n < (BIG ? 4 : 1); ++n)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) big[r][n][i] = 0.f;
-    v4f acc[BIG ? 1 : RT][BIG ? 1 : NT];
-#pragma unroll
-    for (int r = 0; r < (BIG ? 1 : RT); ++r)
-#pragma unroll
-        for (int n = 0; n < (BIG ? 1 : NT); ++n) acc[r][n] = v4f{0.f, 0.f, 0.f, 0.f};
+        for (int n = 0; n < NT; ++n) acc[r][n] = v4f{0.f, 0.f, 0.f, 0.f};
     auto products = [&](int buf, int c, const v4u (&x)[RT]) {
         const v4u* hb = lds + buf * HP + c * NT * (MX4 ? 64 : 256);
-        if constexpr (BIG) {
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const v4u y = hb[at + step(n)];
-#pragma unroll
-                for (int r = n & 1; r < RT; r += 2)
-                    big[r >> 1][n >> 1] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(widen(x[r]), widen(y), big[r >> 1][n >> 1], 4, 4, 0, sw[r] >> (8 * c), 0, sh[n] >> (8 * c));
-            }
-        } else if constexpr (MX4) {
+        if constexpr (MX4) {
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const v4u y = hb[n * 64 + lane];
@@ -331,69 +345,183 @@ __global__ __launch_bounds__(256, NT == 8 ? 2 : 3) void product_kernel(LogitsArg
     for (int c = 0; c < S; ++c)
         if (last * S + c < chunks) products(last & 1, c, w[c]);
 
-    // Output: lane l holds rows 4 (l / 16) .. + 3 of hidden state l % 16 of every tile, or rows 8 i + 4 (l / 32) .. + 3 of hidden state l % 32.
-    // Through LDS, 16 or 32 hidden states at a time, so that a row of logits is written in one piece per wave.
+    // lane l holds rows 4 (l / 16) .. + 3 of hidden state l % 16 of every tile
     __syncthreads();
-    float* buf = (float*)lds + wave * G * OW;
-    const int64_t row0 = tile0 * 16;
+    float* buf = (float*)lds + wave * 16 * OW;
 #pragma unroll
-    for (int n = 0; n < NT * 16 / G; ++n) {
-        const int64_t b0 = htile0 * 16 + n * G;
+    for (int n = 0; n < NT; ++n) {
+        const int64_t b0 = (htile0 + n) * 16;
         if (b0 >= a.B) continue;
-        if constexpr (BIG) {
 #pragma unroll
-            for (int r = 0; r < 2; ++r)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    *(v4f*)(buf + (lane & 31) * OW + r * 32 + i * 8 + (lane >> 5) * 4) = v4f{big[r][n][4 * i], big[r][n][4 * i + 1], big[r][n][4 * i + 2], big[r][n][4 * i + 3]};
-        } else {
-#pragma unroll
-            for (int r = 0; r < RT; ++r) *(v4f*)(buf + col * OW + r * 16 + g * 4) = acc[r][n];
-        }
-        __builtin_amdgcn_wave_barrier();
-        constexpr int W = sizeof(T) == 4 ? 4 : 8;                 // logits in 16 bytes
-        if (a.wide) {
-            constexpr int L = RT * 16 / W;                        // lanes of a hidden state
-            const int64_t row = row0 + lane % L * W;
-            if (row < a.V) {
-                float bias[W];
-#pragma unroll
-                for (int i = 0; i < W; ++i) bias[i] = a.bias ? a.bias[row + i] : 0.f;
-                for (int t = lane / L; t < G && b0 + t < a.B; t += 64 / L) {
-                    float v[W];
-#pragma unroll
-                    for (int i = 0; i < W; ++i) v[i] = buf[t * OW + lane % L * W + i] + bias[i];
-                    T* to = (T*)a.out + (b0 + t) * a.V + row;
-                    if constexpr (sizeof(T) == 4) *(float4*)to = make_float4(v[0], v[1], v[2], v[3]);
-                    else *(v4u*)to = v4u{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
-                }
-            }
-        } else {
-            constexpr int L = RT * 16;
-            const int64_t row = row0 + lane % L;
-            if (row < a.V) {
-                const float bias = a.bias ? a.bias[row] : 0.f;
-                for (int t = lane / L; t < G && b0 + t < a.B; t += 64 / L) {
-                    const float v = buf[t * OW + lane % L] + bias;
-                    T* to = (T*)a.out + (b0 + t) * a.V + row;
-                    if constexpr (sizeof(T) == 4) *to = v;
-                    else *to = __builtin_bit_cast(uint16_t, (__bf16)v);
-                }
-            }
-        }
-        __builtin_amdgcn_wave_barrier();                          // the next group overwrites what this one reads
+        for (int r = 0; r < RT; ++r) *(v4f*)(buf + col * OW + r * 16 + g * 4) = acc[r][n];
+        give_out<16, RT, T>(a, buf, b0, tile0 * 16);
     }
 }
 
+// 256 rows against 128 hidden states in four bits, four waves of 64 rows, where there are enough of both: bound by the matrix cores.
+// 32x32x64 instructions run at 1.7 times the rate of 16x16x128 (6.6 and 3.9 PFLOP/s measured on registers alone, random codes; what holds
+// them at 6.6 is power: codes of zeros reach 8.9).  Lane l of theirs holds a block of row l % 32: two tiles side by side, read in
+// pieces of 256 bytes, blocks l / 32 and then 2 + l / 32 of a step.
+// The blocks that share a band ask for its codes at about the same time, so that each of them waits for memory, not for a cache.  Codes are
+// therefore requested four steps ahead, each register again as soon as its products are issued; h comes two steps at a time, one such
+// stage ahead, from global memory to LDS without registers, which are all taken: 128 sums, 64 of codes.
+template <typename T>
+__global__ __launch_bounds__(256, 2) void many_kernel(LogitsArgs a) {
+    constexpr int OW = 64 + 4;
+    __shared__ v4u lds[4 * 32 * OW / 4 > 2 * 1024 + 256 ? 4 * 32 * OW / 4 : 2 * 1024 + 256];
+    uint32_t* hscale = (uint32_t*)(lds + 2 * 1024);               // two buffers of 8 tiles
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int j = blockIdx.x >> 3, group = j % a.groups, block = (j / a.groups) * 8 + (blockIdx.x & 7);
+    if (block >= a.blocks) return;
+    const int chunks = a.chunks, quads = (chunks + 3) >> 2;
+    const int at = (lane >> 4 & 1) * 64 + (lane >> 5) * 16 + (lane & 15);      // this lane's block in a run of tiles, in lanes
+    auto step = [](int r) { return (r >> 1) * 128 + (r & 1) * 32; };           // and from there to register r: tiles 2 (r / 2), blocks 2 (r % 2)
+    const uint8_t* band = a.bands + ((int64_t)block * 4 + wave) * band_bytes(chunks);
+    const int64_t htile0 = (int64_t)group * 8;
+    // addresses: a scalar for the wave and 32 bits for the lane
+    const uint8_t* hc = a.hc + (htile0 + wave) * chunks * 1024;
+    const uint8_t* hs = (const uint8_t*)a.hs + (htile0 + wave) * quads * 256;
+    const uint32_t at16 = at * 16, at4 = at * 4, lane16 = lane * 16, lane4 = lane * 4;
+
+    v4u w[4][4];
+    uint32_t sw[4], sw_next[4];
+    auto load_w = [&](int c, v4u (&to)[4]) {
+        const uint8_t* p = band + codes_at(min(c, chunks - 1));
+#pragma unroll
+        for (int r = 0; r < 4; ++r) to[r] = *(const v4u*)(p + (at16 + step(r) * 16));
+    };
+    auto load_scales = [&](int q) {
+        q = min(q, quads - 1);
+        const uint8_t* p = band + scales_at(q);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sw_next[r] = *(const uint32_t*)(p + (at4 + step(r) * 4));
+    };
+    // h goes past the registers: wave w brings tiles w and w + 4, of two steps, or their scales of four.  (Buffer loads: global loads to LDS count
+    // as loads that may touch either memory, and then every wait for a register waits for all of them.)
+    typedef __attribute__((address_space(3))) void* lds_ptr;
+    const auto h_rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)hc, 0, 5 * chunks * 1024, 0x00027000);      // raw bytes, checked against the last tile's end
+    const auto hs_rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)hs, 0, 5 * quads * 256, 0x00027000);
+    auto load_h = [&](int c0, int buf) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(h_rsrc, (lds_ptr)(lds + buf * 1024 + (i >> 1) * 512 + (i & 1) * 256 + wave * 64), 16, lane16,
+                                                     ((i & 1) * 4 * chunks + min(c0 + (i >> 1), chunks - 1)) * 1024, 0, 0);
+    };
+    auto load_hscales = [&](int q) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(hs_rsrc, (lds_ptr)(hscale + (q & 1) * 512 + i * 256 + wave * 64), 4, lane4,
+                                                     (i * 4 * quads + min(q, quads - 1)) * 256, 0, 0);
+    };
+    v16f acc[2][4];
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[r][n][i] = 0.f;
+    auto products = [&](auto step_c, int q, const v4u (&x)[4]) {
+        constexpr int c = decltype(step_c)::value;
+        const v4u* hb = lds + (c >> 1) * 1024 + (c & 1) * 512;
+        const uint32_t* sb = hscale + (q & 1) * 512;
+#pragma unroll
+        for (int n = 0; n < 8; ++n) {
+            const v4u y = hb[at + step(n)];
+            const uint32_t sy = sb[at + step(n)];
+#pragma unroll
+            for (int r = n & 1; r < 4; r += 2)
+                acc[r >> 1][n >> 1] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(widen(x[r]), widen(y), acc[r >> 1][n >> 1], 4, 4, c, sw[r], c, sy);
+        }
+    };
+    // A stage of two steps: its h is in LDS, the next one's requested.  The eight loads of codes that follow h's are the youngest ones: waiting
+    // for all but eight waits for h (and for the codes of this stage), not for codes of later ones.
+    auto begin = [&](int q, int half, bool more) {
+        // (A fence in place of the barrier's memory clobber would wait for all loads, because those of h write LDS.)
+        if (more || half == 0) asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");      // nothing has been asked for after h
+        if (half == 0) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sw[r] = sw_next[r];
+        }
+        if (more || half == 0) load_h(4 * q + 2 * half + 2, half ^ 1);
+        if (more && half == 0) {
+            load_hscales(q + 1);
+            load_scales(q + 1);
+        }
+        __builtin_amdgcn_sched_barrier(0);                        // requests stay where they are written
+    };
+    load_h(0, 0);
+    load_hscales(0);
+    load_scales(0);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) load_w(c, w[c]);
+    for (int q = 0; q < quads - 1; ++q) {
+        begin(q, 0, true);
+        products(std::integral_constant<int, 0>(), q, w[0]);
+        load_w(4 * q + 4, w[0]);
+        __builtin_amdgcn_sched_barrier(0);
+        products(std::integral_constant<int, 1>(), q, w[1]);
+        load_w(4 * q + 5, w[1]);
+        __builtin_amdgcn_sched_barrier(0);
+        begin(q, 1, true);
+        products(std::integral_constant<int, 2>(), q, w[2]);
+        load_w(4 * q + 6, w[2]);
+        __builtin_amdgcn_sched_barrier(0);
+        products(std::integral_constant<int, 3>(), q, w[3]);
+        load_w(4 * q + 7, w[3]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    const int last = quads - 1, left = chunks - 4 * last;         // the last steps ask for nothing more
+    begin(last, 0, false);
+    products(std::integral_constant<int, 0>(), last, w[0]);
+    if (left > 1) products(std::integral_constant<int, 1>(), last, w[1]);
+    if (left > 2) {
+        begin(last, 1, false);
+        products(std::integral_constant<int, 2>(), last, w[2]);
+        if (left > 3) products(std::integral_constant<int, 3>(), last, w[3]);
+    }
+
+    // lane l holds rows 8 i + 4 (l / 32) .. + 3 of hidden state l % 32 of a block of 32 x 32
+    __syncthreads();
+    float* buf = (float*)lds + wave * 32 * OW;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        const int64_t b0 = htile0 * 16 + n * 32;
+        if (b0 >= a.B) continue;
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *(v4f*)(buf + (lane & 31) * OW + r * 32 + i * 8 + (lane >> 5) * 4) = v4f{acc[r][n][4 * i], acc[r][n][4 * i + 1], acc[r][n][4 * i + 2], acc[r][n][4 * i + 3]};
+        give_out<32, 4, T>(a, buf, b0, ((int64_t)block * 4 + wave) * 64);
+    }
+}
+
+// blocks of the grid for tiles of `rows` x `states`, or 0 where they are too many
+static unsigned plan(LogitsArgs& a, int rows, int states) {
+    a.blocks = (a.V + rows - 1) / rows;
+    a.groups = (a.B + states - 1) / states;
+    const int64_t n = (int64_t)(a.blocks + 7) / 8 * 8 * a.groups;
+    if (n <= 0x7fffffff) return (unsigned)n;
+    csv_set_error("V=%d rows x B=%d hidden states are too many blocks", a.V, a.B);
+    return 0;
+}
 template <bool MX4, int NT, int RT, int S>
 static int launch_product(LogitsArgs a, int out_type, hipStream_t st) {
-    a.blocks = (a.V + 64 * RT - 1) / (64 * RT);
-    a.groups = (a.B + NT * 16 - 1) / (NT * 16);
-    const int64_t n = (int64_t)(a.blocks + 7) / 8 * 8 * a.groups;
-    if (n > 0x7fffffff) { csv_set_error("V=%d rows x B=%d hidden states are too many blocks", a.V, a.B); return CSV_ESHAPE; }
-    if (out_type == CSV_F32) product_kernel<MX4, NT, RT, S, float><<<(unsigned)n, 256, 0, st>>>(a);
-    else product_kernel<MX4, NT, RT, S, uint16_t><<<(unsigned)n, 256, 0, st>>>(a);
+    const unsigned n = plan(a, 64 * RT, 16 * NT);
+    if (!n) return CSV_ESHAPE;
+    if (out_type == CSV_F32) product_kernel<MX4, NT, RT, S, float><<<n, 256, 0, st>>>(a);
+    else product_kernel<MX4, NT, RT, S, uint16_t><<<n, 256, 0, st>>>(a);
     CSV_LAUNCH_CHECK("product_kernel");
+    return CSV_OK;
+}
+static int launch_many(LogitsArgs a, int out_type, hipStream_t st) {
+    const unsigned n = plan(a, 256, 128);
+    if (!n) return CSV_ESHAPE;
+    if (out_type == CSV_F32) many_kernel<float><<<n, 256, 0, st>>>(a);
+    else many_kernel<uint16_t><<<n, 256, 0, st>>>(a);
+    CSV_LAUNCH_CHECK("many_kernel");
     return CSV_OK;
 }
 
@@ -441,7 +569,7 @@ extern "C" int csv_mx4_head_create(const uint8_t* d_codes, const uint8_t* d_scal
     *out = nullptr;
     if (!d_codes || !d_scales) { csv_set_error("null codes or scales"); return CSV_EINVAL; }
     if (V < 1 || d < 8 || (d & 7) != 0) { csv_set_error("need V >= 1 and d a positive multiple of 8 (V=%d, d=%d)", V, d); return CSV_ESHAPE; }
-    if (V > 0x7fffffff - HEAD_ROWS) { csv_set_error("V=%d is too large", V); return CSV_ESHAPE; }
+    if (V > 0x7fffffff - HEAD_ROWS || d > CSV_MX4_MAX_D) { csv_set_error("V=%d or d=%d is too large", V, d); return CSV_ESHAPE; }
     if ((uintptr_t)d_codes & 15) { csv_set_error("codes have to be 16-byte aligned"); return CSV_EINVAL; }
     csv_mx4_head* x = (csv_mx4_head*)calloc(1, sizeof(csv_mx4_head));
     if (!x) { csv_set_error("host allocation failed"); return CSV_ENOMEM; }
@@ -548,5 +676,5 @@ extern "C" int csv_mx4_logits(const csv_mx4_head* x, const uint16_t* d_h, int B,
     if (B <= 32) return launch_product<true, 2, 2, 4>(a, out_type, st);
     if (B <= 64) return full >= fill ? launch_product<true, 4, 4, 1>(a, out_type, st) : launch_product<true, 4, 2, 2>(a, out_type, st);
     // 100 hidden states: 24000 x 4096, 28.8 against 23.9 in groups of 64; 60000 x 2048, 22.7 against 26.8
-    return full * ((B + 127) / 128) >= fill / 2 ? launch_product<true, 8, 4, 2>(a, out_type, st) : launch_product<true, 4, 2, 2>(a, out_type, st);
+    return full * ((B + 127) / 128) >= fill / 2 ? launch_many(a, out_type, st) : launch_product<true, 4, 2, 2>(a, out_type, st);
 }

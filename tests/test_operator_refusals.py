@@ -46,7 +46,7 @@ def test_head_and_logits_refused(csv):
     for args in ((None, P, None, 16, 64), (P, None, None, 16, 64), (P + 4, P, None, 16, 64)):
         out.value = 77
         assert make(*args, None, C.byref(out)) == EINVAL and out.value is None
-    for V, d in ((0, 64), (16, 0), (16, 63), (2 ** 31 - 1, 64)):
+    for V, d in ((0, 64), (16, 0), (16, 63), (2 ** 31 - 1, 64), (16, 2 ** 20 + 8)):
         out.value = 77
         assert make(P, P, None, V, d, None, C.byref(out)) == ESHAPE and out.value is None
     n = C.c_size_t()

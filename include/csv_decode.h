@@ -366,9 +366,9 @@ int csv_mx4_logits(const csv_mx4_head* head, const uint16_t* d_h, int B, int act
  * with a NaN or a plus infinity gives NaN.
  * csv_token_logprobs_backward: d_grad[i, j] = c g_i ([j = t] - exp(c (x_j - m)) / s) for g = d_grad_logp, in the type of the
  * logits, from the d_stats of the forward call; d_grad may be d_logits (then ld_grad = ld).  A row with g_i = 0 is zeros and
- * is not read.  Scratch: csv_loss_scratch bytes, 16-byte aligned, for the forward call.
+ * is not read.  Scratch: csv_token_logprobs_scratch bytes, 16-byte aligned, for the forward call (often none).
  */
-int csv_loss_scratch(int N, int V, size_t* bytes);
+int csv_token_logprobs_scratch(int N, int V, size_t* bytes);
 int csv_token_logprobs(const void* d_logits, int type, int64_t ld, int N, int V, const int32_t* d_tokens, float inv_temperature,
                        float* d_logp, float* d_stats, void* d_scratch, size_t scratch_bytes, void* stream);
 int csv_token_logprobs_backward(const void* d_logits, int type, int64_t ld, int N, int V, const int32_t* d_tokens,
@@ -385,6 +385,7 @@ int csv_token_logprobs_backward(const void* d_logits, int type, int64_t ld, int 
  * ld).  A row of weight 0, or of a token outside 0..V-1, is left out: nothing of it is read, d_logp 0, a gradient row of zeros.
  * A row of minus infinities has logp minus infinity and a gradient row of zeros.  d_ref_logp is not read where beta is 0.
  * The sum over rows is in float64 and in one order: equal calls (with rows at equal alignments) give equal bits.
+ * Scratch: csv_policy_loss_scratch bytes, 16-byte aligned.
  */
 typedef struct {
     float clip_low;        /* 0..1 */
@@ -392,6 +393,7 @@ typedef struct {
     float beta;            /* >= 0, finite */
     float inv_temperature; /* > 0, finite */
 } csv_policy_params;
+int csv_policy_loss_scratch(int N, int V, size_t* bytes);
 int csv_policy_loss(const void* d_logits, int type, int64_t ld, int N, int V, const int32_t* d_tokens,
                     const float* d_old_logp, const float* d_ref_logp, const float* d_advantages, const float* d_weights,
                     const csv_policy_params* params, float* d_loss, float* d_logp, void* d_grad, int64_t ld_grad,

@@ -32,8 +32,8 @@ EXPORTS = [
     "csv_workspace_set_tail_split", "csv_bounds_static", "csv_index_set_bias_table", "csv_index_get_bias_table",
     "csv_index_set_angular", "csv_index_get_angular",
     "csv_mx4_quantize", "csv_mx4_dequantize", "csv_mx4_head_create", "csv_mx4_head_dims", "csv_mx4_head_free",
-    "csv_mx4_logits_scratch", "csv_mx4_logits", "csv_loss_scratch", "csv_token_logprobs", "csv_token_logprobs_backward",
-    "csv_policy_loss",
+    "csv_mx4_logits_scratch", "csv_mx4_logits", "csv_token_logprobs_scratch", "csv_token_logprobs",
+    "csv_token_logprobs_backward", "csv_policy_loss_scratch", "csv_policy_loss",
 ]
 PROFILE_STAGES = ["bounds", "round0", "tail"]
 
@@ -105,7 +105,8 @@ def _load() -> C.CDLL:
     lib.csv_mx4_head_free.restype = None
     lib.csv_mx4_logits_scratch.argtypes = [vp, ci, ci, C.POINTER(sz)]
     lib.csv_mx4_logits.argtypes = [vp, vp, ci, ci, vp, ci, vp, sz, vp]
-    lib.csv_loss_scratch.argtypes = [ci, ci, C.POINTER(sz)]
+    lib.csv_token_logprobs_scratch.argtypes = [ci, ci, C.POINTER(sz)]
+    lib.csv_policy_loss_scratch.argtypes = [ci, ci, C.POINTER(sz)]
     lib.csv_token_logprobs.argtypes = [vp, ci, i64, ci, ci, vp, cf, vp, vp, vp, sz, vp]
     lib.csv_token_logprobs_backward.argtypes = [vp, ci, i64, ci, ci, vp, vp, vp, cf, vp, i64, vp]
     lib.csv_policy_loss.argtypes = [vp, ci, i64, ci, ci, vp, vp, vp, vp, vp, C.POINTER(PolicyParams), vp, vp, vp, i64, vp, sz, vp]
@@ -530,10 +531,18 @@ def csv_mx4_logits(head: CsvMx4Head, h: torch.Tensor, out: torch.Tensor | None =
 
 
 @functools.lru_cache(maxsize=256)
-def csv_loss_scratch(N: int, V: int) -> int:
-    """Bytes of scratch that csv_token_logprobs and csv_policy_loss need for logits [N, V]."""
+def csv_token_logprobs_scratch(N: int, V: int) -> int:
+    """Bytes of scratch that csv_token_logprobs needs for logits [N, V]."""
     need = C.c_size_t()
-    _check(lib.csv_loss_scratch(N, V, C.byref(need)))
+    _check(lib.csv_token_logprobs_scratch(N, V, C.byref(need)))
+    return need.value
+
+
+@functools.lru_cache(maxsize=256)
+def csv_policy_loss_scratch(N: int, V: int) -> int:
+    """Bytes of scratch that csv_policy_loss needs for logits [N, V]."""
+    need = C.c_size_t()
+    _check(lib.csv_policy_loss_scratch(N, V, C.byref(need)))
     return need.value
 
 
@@ -549,7 +558,7 @@ def csv_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, inv_temperatu
         logp = torch.empty(N, dtype=torch.float32, device=dev)
     if stats is None:
         stats = torch.empty((N, 2), dtype=torch.float32, device=dev)
-    keep, ptr, size = _scratch(csv_loss_scratch(N, V), scratch, dev)
+    keep, ptr, size = _scratch(csv_token_logprobs_scratch(N, V), scratch, dev)
     _check(lib.csv_token_logprobs(logits.data_ptr(), ty, ld, N, V, _dense(tokens, "tokens", torch.int32, (N,), dev), inv_temperature,
                                   _dense(logp, "logp", torch.float32, (N,), dev), _dense(stats, "stats", torch.float32, (N, 2), dev), ptr, size,
                                   torch._C._cuda_getCurrentRawStream(dev)))
@@ -601,7 +610,7 @@ def csv_policy_loss(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.
     if grad is None and want_grad:
         grad = torch.empty((N, V), dtype=logits.dtype, device=dev)
     gp, gld = (None, 0) if grad is None else _grad_of(logits, grad, ty, dev)
-    keep, ptr, size = _scratch(csv_loss_scratch(N, V), scratch, dev)
+    keep, ptr, size = _scratch(csv_policy_loss_scratch(N, V), scratch, dev)
     _check(lib.csv_policy_loss(logits.data_ptr(), ty, ld, N, V, _dense(tokens, "tokens", torch.int32, n, dev), _dense(old_logp, "old_logp", f32, n, dev),
                                None if ref_logp is None else _dense(ref_logp, "ref_logp", f32, n, dev), _dense(advantages, "advantages", f32, n, dev),
                                _dense(weights, "weights", f32, n, dev), C.byref(PolicyParams(clip_low, clip_high, beta, inv_temperature)),

@@ -402,10 +402,7 @@ static int check_grad(const void* x, int type, int64_t ld, int N, int V, const v
     if (N > 1 && grad == x && ld_grad != ld) { csv_set_error("a gradient in place of the logits needs their row stride"); return CSV_EINVAL; }
     return CSV_OK;
 }
-static int check_scratch(int N, int V, const void* p, size_t have) {
-    size_t need = 0;
-    const int rc = csv_loss_scratch(N, V, &need);
-    if (rc) return rc;
+static int check_scratch(size_t need, const void* p, size_t have) {
     if (need && (!p || have < need)) { csv_set_error("scratch of %zu bytes, %zu are needed", p ? have : (size_t)0, need); return CSV_ESHAPE; }
     if (need && ((uintptr_t)p & 15)) { csv_set_error("scratch has to be 16-byte aligned"); return CSV_EINVAL; }
     return CSV_OK;
@@ -426,11 +423,20 @@ static inline int parts_of(int N, int V, int most) {
     return p < 1 ? 1 : p > MAX_PARTS ? MAX_PARTS : p;
 }
 
-extern "C" int csv_loss_scratch(int N, int V, size_t* bytes) {
+static int scratch_bytes(int N, int V, bool parts, size_t* bytes) {
     if (N < 0 || V < 1) { csv_set_error("need N >= 0 and V >= 1 (N=%d, V=%d)", N, V); return CSV_ESHAPE; }
     if (!bytes) { csv_set_error("null bytes"); return CSV_EINVAL; }
-    *bytes = (size_t)N * sizeof(double) + (N > 0 && N < FEW_ROWS ? (size_t)N * (sizeof(float2) * parts_of(N, V, PART_BLOCKS) + 8) + 8 : 0);
+    *bytes = (size_t)N * sizeof(double) + (parts && N > 0 ? (size_t)N * (sizeof(float2) * parts_of(N, V, PART_BLOCKS) + 8) + 8 : 0);
     return CSV_OK;
+}
+static inline bool logprobs_by_parts(int N, int V) { return N < FEW_ROWS && V > LONG_ROW; }
+
+extern "C" int csv_policy_loss_scratch(int N, int V, size_t* bytes) { return scratch_bytes(N, V, N < FEW_ROWS, bytes); }
+
+extern "C" int csv_token_logprobs_scratch(int N, int V, size_t* bytes) {
+    const int rc = scratch_bytes(N, V, logprobs_by_parts(N, V), bytes);
+    if (!rc && !logprobs_by_parts(N, V)) *bytes = 0;
+    return rc;
 }
 
 static void place_scratch(RowArgs& a, void* p) {
@@ -443,15 +449,17 @@ static void place_scratch(RowArgs& a, void* p) {
 }
 
 extern "C" int csv_token_logprobs(const void* d_logits, int type, int64_t ld, int N, int V, const int32_t* d_tokens, float inv_temperature, float* d_logp,
-                                  float* d_stats, void* d_scratch, size_t scratch_bytes, void* stream) {
+                                  float* d_stats, void* d_scratch, size_t have, void* stream) {
     int rc = check_logits(d_logits, type, ld, N, V, d_tokens, inv_temperature);
-    if (!rc) rc = check_scratch(N, V, d_scratch, scratch_bytes);
+    size_t need = 0;
+    if (!rc) rc = csv_token_logprobs_scratch(N, V, &need);
+    if (!rc) rc = check_scratch(need, d_scratch, have);
     if (rc || N == 0) return rc;
     if (!d_logp || !d_stats) { csv_set_error("null d_logp or d_stats"); return CSV_EINVAL; }
     RowArgs a = {};
     a.x = d_logits; a.ld = ld; a.N = N; a.V = V; a.tokens = d_tokens; a.c = inv_temperature; a.logp = d_logp; a.stats = d_stats;
     const hipStream_t st = (hipStream_t)stream;
-    if (N < FEW_ROWS && V > LONG_ROW) {
+    if (logprobs_by_parts(N, V)) {
         place_scratch(a, d_scratch);
         if (type == CSV_F32) part_kernel<float, false><<<N * a.parts, 256, 0, st>>>(a);
         else part_kernel<uint16_t, false><<<N * a.parts, 256, 0, st>>>(a);
@@ -486,11 +494,13 @@ extern "C" int csv_token_logprobs_backward(const void* d_logits, int type, int64
 
 extern "C" int csv_policy_loss(const void* d_logits, int type, int64_t ld, int N, int V, const int32_t* d_tokens, const float* d_old_logp,
                                const float* d_ref_logp, const float* d_advantages, const float* d_weights, const csv_policy_params* p, float* d_loss,
-                               float* d_logp, void* d_grad, int64_t ld_grad, void* d_scratch, size_t scratch_bytes, void* stream) {
+                               float* d_logp, void* d_grad, int64_t ld_grad, void* d_scratch, size_t have, void* stream) {
     if (!p || !d_loss) { csv_set_error("null params or d_loss"); return CSV_EINVAL; }
     int rc = check_logits(d_logits, type, ld, N, V, d_tokens, p->inv_temperature);
     if (!rc && d_grad) rc = check_grad(d_logits, type, ld, N, V, d_grad, ld_grad);
-    if (!rc) rc = check_scratch(N, V, d_scratch, scratch_bytes);
+    size_t need = 0;
+    if (!rc) rc = csv_policy_loss_scratch(N, V, &need);
+    if (!rc) rc = check_scratch(need, d_scratch, have);
     if (rc) return rc;
     if (!(p->clip_low >= 0.f && p->clip_low <= 1.f) || !(p->clip_high >= 0.f)) { csv_set_error("clip range 1 - %g .. 1 + %g", (double)p->clip_low, (double)p->clip_high); return CSV_EINVAL; }
     if (!(p->beta >= 0.f) || !isfinite(p->beta)) { csv_set_error("beta=%g is negative or not finite", (double)p->beta); return CSV_EINVAL; }

@@ -59,13 +59,17 @@ def test_head_and_logits_refused(csv):
 
 def test_loss_refused(csv):
     n = C.c_size_t()
-    assert csv.lib.csv_loss_scratch(-1, 5, C.byref(n)) == ESHAPE
-    assert csv.lib.csv_loss_scratch(1, 0, C.byref(n)) == ESHAPE
-    assert csv.lib.csv_loss_scratch(1, 5, None) == EINVAL
-    assert csv.lib.csv_loss_scratch(3, 70000, C.byref(n)) == 0 and n.value >= 24
+    for f in (csv.lib.csv_token_logprobs_scratch, csv.lib.csv_policy_loss_scratch):
+        assert f(-1, 5, C.byref(n)) == ESHAPE
+        assert f(1, 0, C.byref(n)) == ESHAPE
+        assert f(1, 5, None) == EINVAL
+        assert f(3, 70000, C.byref(n)) == 0 and n.value >= 24
+        assert f(0, 70000, C.byref(n)) == 0 and n.value == 0
+    assert csv.lib.csv_policy_loss_scratch(3, 100, C.byref(n)) == 0 and n.value >= 24
+    assert csv.lib.csv_token_logprobs_scratch(3, 100, C.byref(n)) == 0 and n.value == 0
     big = 1 << 40
 
-    def fwd(x=P, ty=0, ld=100, N=3, V=100, t=P, c=1.0, logp=P, stats=P, scr=P, size=big):
+    def fwd(x=P, ty=0, ld=70000, N=3, V=70000, t=P, c=1.0, logp=P, stats=P, scr=P, size=big):
         return csv.lib.csv_token_logprobs(x, ty, ld, N, V, t, c, logp, stats, scr, size, None)
 
     def bwd(x=P, ty=0, ld=100, N=3, V=100, t=P, stats=P, g=P, c=1.0, grad=2 * P, ldg=100):
@@ -79,7 +83,7 @@ def test_loss_refused(csv):
     for f in (fwd, bwd, pol):
         assert f(N=-1) == ESHAPE
         assert f(V=0) == ESHAPE
-        assert f(ld=99) == ESHAPE
+        assert f(ld=99, V=100) == ESHAPE
         assert f(ty=7) == EINVAL
         assert f(x=None) == EINVAL
         assert f(t=None) == EINVAL

@@ -325,7 +325,8 @@ int csv_kmax_update(csv_kmax_ctl* c, int n_fallback, int n_sequences);
  * (ties to the even index, magnitudes above 6 to 6), as four bits: sign, then the index in that list.  The even element
  * of a pair is the low half of its byte.  A block with a NaN or an infinity has the scale byte 255 and stands for NaNs.
  * d_codes uint8[rows * dp/2] (16-byte aligned), d_scales uint8[rows * dp/32] (4-byte aligned), both row-major.
- * csv_mx4_quantize: d_x [rows, d] of x_type with ld elements from one row to the next (ld >= d, ld % 8 == 0), 16-byte aligned.
+ * csv_mx4_quantize: d_x [rows, d] of x_type with ld elements from one row to the next (ld >= d, ld % 8 == 0), 16-byte aligned;
+ * rows and d at most 2^30.
  * csv_mx4_dequantize writes the values that the rows stand for (exact in both types; beyond the type's range: infinite).
  */
 int csv_mx4_quantize(const void* d_x, int x_type, int64_t ld, int rows, int d, uint8_t* d_codes, uint8_t* d_scales, void* stream);

@@ -95,15 +95,16 @@ __global__ __launch_bounds__(256) void quantize_kernel(const T* __restrict__ x, 
     }
 }
 
+// values leave past the caches: four times what came in, and read by another kernel at the earliest
 __device__ __forceinline__ void store8(float* p, const float* v) {
-    ((float4*)p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-    ((float4*)p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    __builtin_nontemporal_store(v4f{v[0], v[1], v[2], v[3]}, (v4f*)p);
+    __builtin_nontemporal_store(v4f{v[4], v[5], v[6], v[7]}, (v4f*)p + 1);
 }
 // the values have two significant bits: the high half of the float32 pattern is the bfloat16
 __device__ __forceinline__ void store8(uint16_t* p, const float* v) {
     uint32_t w[4];
     for (int j = 0; j < 4; ++j) w[j] = (__float_as_uint(v[2 * j]) >> 16) | (__float_as_uint(v[2 * j + 1]) & 0xffff0000u);
-    *(uint4*)p = make_uint4(w[0], w[1], w[2], w[3]);
+    __builtin_nontemporal_store(v4u{w[0], w[1], w[2], w[3]}, (v4u*)p);
 }
 template <typename T>
 __global__ __launch_bounds__(256) void dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int rows, int d, int chunks,
@@ -528,6 +529,7 @@ static int launch_many(LogitsArgs a, int out_type, hipStream_t st) {
 // ------------------------------------------------------------------------------------------------ entry points
 static int check_rows(int rows, int d, int type, int64_t ld, const void* x, const uint8_t* codes, const uint8_t* scales) {
     if (rows < 0 || d < 8 || (d & 7) != 0) { csv_set_error("need rows >= 0 and d a positive multiple of 8 (rows=%d, d=%d)", rows, d); return CSV_ESHAPE; }
+    if (rows > 1 << 30 || d > 1 << 30) { csv_set_error("rows=%d or d=%d is above 2^30", rows, d); return CSV_ESHAPE; }
     if (type != CSV_F32 && type != CSV_BF16) { csv_set_error("bad element type %d", type); return CSV_EINVAL; }
     if (ld < d || (ld & 7) != 0) { csv_set_error("row stride %lld is below d=%d or no multiple of 8", (long long)ld, d); return CSV_ESHAPE; }
     if (rows == 0) return CSV_OK;

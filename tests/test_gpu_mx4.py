@@ -64,8 +64,30 @@ def test_quantize_every_code(R, d, dtype, gap):
         assert (got[:, d:] == 7.0).all()
 
 
-@pytest.mark.parametrize("dtype,top", [(BF16, 3.4e38), (F32, 3.41e38)])
-def test_dequantize_every_code_at_every_scale(dtype, top):
+@pytest.mark.parametrize("R,d", [(140003, 40), (3, 2400008)])
+def test_quantize_many_rows_and_long_rows(R, d):
+    """More rows than a grid has blocks for, and a row as long as a flattened matrix: pieces of 40 elements from a list, each rounded as in the list."""
+    csv = _csv()
+    log(f"quantize R={R} d={d}")
+    gen = torch.Generator().manual_seed(R)
+    base = (torch.randn(64, 40, generator=gen) * torch.exp(2 * torch.randn(64, 1, generator=gen))).to(BF16)
+    if R > 1000:
+        pick = torch.randint(0, 64, (R,), generator=gen)
+        want_c, want_s = O.mx4_quantize(O.bf16_values(base))
+        codes, scales = csv.csv_mx4_quantize(base[pick].cuda())
+        assert np.array_equal(codes.cpu().numpy(), want_c[pick]) and np.array_equal(scales.cpu().numpy(), want_s[pick])
+        return
+    x = base.reshape(-1)[torch.arange(R * d) % 2560].reshape(R, d)
+    codes, scales = csv.csv_mx4_quantize(x.cuda())
+    for lo in (0, 1024, d // 128 // 2 * 128, d - d % 128):         # a stretch of 128 elements at a time
+        hi = min(d, lo + 128)
+        want_c, want_s = O.mx4_quantize(O.bf16_values(x[:, lo:hi]))
+        assert np.array_equal(codes[:, lo // 2:lo // 2 + 64].cpu().numpy(), want_c)
+        assert np.array_equal(scales[:, lo // 32:lo // 32 + 4].cpu().numpy(), want_s)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_dequantize_every_code_at_every_scale(dtype):
     csv = _csv()
     codes = torch.arange(256, dtype=torch.int64).to(torch.uint8).repeat(256, 1).cuda()          # 512 codes a row: all pairs
     scales = torch.arange(256, dtype=torch.int64).to(torch.uint8)[:, None].repeat(1, 16).cuda()

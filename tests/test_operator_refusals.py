@@ -27,6 +27,8 @@ def test_rows_refused(csv):
         assert f(P, csv.BF16, 64, -1, 64, P, P) == ESHAPE
         assert f(P, csv.BF16, 64, 4, 0, P, P) == ESHAPE
         assert f(P, csv.BF16, 64, 4, 60, P, P) == ESHAPE           # d is no multiple of 8
+        assert f(P, csv.BF16, 64, 2 ** 30 + 1, 64, P, P) == ESHAPE
+        assert f(P, csv.BF16, 2 ** 31, 4, 2 ** 30 + 8, P, P) == ESHAPE
         assert f(P, csv.BF16, 56, 4, 64, P, P) == ESHAPE           # stride below d
         assert f(P, csv.BF16, 68, 4, 64, P, P) == ESHAPE           # stride no multiple of 8
         assert f(P, 2, 64, 4, 64, P, P) == EINVAL                  # unknown type

@@ -180,7 +180,8 @@ __device__ __forceinline__ void lds_barrier() {
 }
 
 // The logits of G hidden states from b0 on and RT * 16 rows from row0 on, from a wave's part of LDS, where a hidden state is a row: so
-// that a row of logits is written in one piece per wave.
+// that a row of logits is written in one piece per wave.  Logits leave past the caches, which keep W and h (us, without / with: 32 hidden states
+// at 256000 x 4608, float32, 131 / 117; 2048 at 128257 x 1024, 655 / 568).
 template <int G, int RT, typename T>
 __device__ __forceinline__ void give_out(const LogitsArgs& a, const float* buf, int64_t b0, int64_t row0) {
     constexpr int OW = RT * 16 + 4;
@@ -199,8 +200,8 @@ __device__ __forceinline__ void give_out(const LogitsArgs& a, const float* buf, 
 #pragma unroll
                 for (int i = 0; i < W; ++i) v[i] = buf[t * OW + lane % L * W + i] + bias[i];
                 T* to = (T*)a.out + (b0 + t) * a.V + row;
-                if constexpr (sizeof(T) == 4) *(float4*)to = make_float4(v[0], v[1], v[2], v[3]);
-                else *(v4u*)to = v4u{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+                if constexpr (sizeof(T) == 4) __builtin_nontemporal_store(v4f{v[0], v[1], v[2], v[3]}, (v4f*)to);
+                else __builtin_nontemporal_store(v4u{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])}, (v4u*)to);
             }
         }
     } else {
@@ -211,12 +212,20 @@ __device__ __forceinline__ void give_out(const LogitsArgs& a, const float* buf, 
             for (int t = lane / L; t < G && b0 + t < a.B; t += 64 / L) {
                 const float v = buf[t * OW + lane % L] + bias;
                 T* to = (T*)a.out + (b0 + t) * a.V + row;
-                if constexpr (sizeof(T) == 4) *to = v;
+                if constexpr (sizeof(T) == 4) __builtin_nontemporal_store(v, to);
                 else *to = __builtin_bit_cast(uint16_t, (__bf16)v);
             }
         }
     }
     __builtin_amdgcn_wave_barrier();                              // the next group overwrites what this one reads
+}
+
+// Codes that one block alone reads (ONCE: all hidden states in one group) go past the caches: 1 hidden state at 128256 x 4096 53.0 -> 46.4 us, 32 at
+// 256000 x 4608 117 -> 107; where several blocks read them it costs as much (2048 at 128256 x 4096 in bf16 1695 -> 1861).
+template <bool ONCE>
+__device__ __forceinline__ v4u load_codes(const uint8_t* p) {
+    if constexpr (ONCE) return __builtin_nontemporal_load((const v4u*)p);
+    else return *(const v4u*)p;
 }
 
 // Four waves, RT tiles of 16 rows each, against NT groups of 16 hidden states; K goes by in stages of S tiles of 128.
@@ -227,7 +236,7 @@ __device__ __forceinline__ void give_out(const LogitsArgs& a, const float* buf, 
 // stage of h lies in LDS, two buffers, and passes through registers on its way there, so that a barrier waits for no load.  bf16 h lies row by
 // row with the 16-byte pieces of row t exchanged by t % 16 (a column of pieces then spreads over all banks); 4-bit h lies as its tiles.
 // Past the end of a row or of the batch the last piece or row is read again: codes of W are 0 there, and those hidden states are not stored.
-template <bool MX4, int NT, int RT, int S, typename T>
+template <bool MX4, int NT, int RT, int S, bool ONCE, typename T>
 __global__ __launch_bounds__(256, 3) void product_kernel(LogitsArgs a) {
     constexpr int HP = NT * S * (MX4 ? 64 : 256);                 // 16-byte pieces of a stage of h
     constexpr int HT = (HP + 255) / 256;                          // of them per thread
@@ -250,7 +259,7 @@ __global__ __launch_bounds__(256, 3) void product_kernel(LogitsArgs a) {
     auto load_w = [&](int c, v4u (&to)[RT]) {
         const int cc = min(c, chunks - 1);
 #pragma unroll
-        for (int r = 0; r < RT; ++r) to[r] = *(const v4u*)(wc + codes_at(cc) + r * 1024);
+        for (int r = 0; r < RT; ++r) to[r] = load_codes<ONCE>(wc + codes_at(cc) + r * 1024);
     };
     auto load_scales = [&](int c0) {                              // a stage lies within four tiles
         const int q = min(c0, chunks - 1) >> 2;
@@ -366,7 +375,7 @@ __global__ __launch_bounds__(256, 3) void product_kernel(LogitsArgs a) {
 // The blocks that share a band ask for its codes at about the same time, so that each of them waits for memory, not for a cache.  Codes are
 // therefore requested four steps ahead, each register again as soon as its products are issued; h comes two steps at a time, one such
 // stage ahead, from global memory to LDS without registers, which are all taken: 128 sums, 64 of codes.
-template <typename T>
+template <bool ONCE, typename T>
 __global__ __launch_bounds__(256, 2) void many_kernel(LogitsArgs a) {
     constexpr int OW = 64 + 4;
     __shared__ v4u lds[4 * 32 * OW / 4 > 2 * 1024 + 256 ? 4 * 32 * OW / 4 : 2 * 1024 + 256];
@@ -389,7 +398,7 @@ __global__ __launch_bounds__(256, 2) void many_kernel(LogitsArgs a) {
     auto load_w = [&](int c, v4u (&to)[4]) {
         const uint8_t* p = band + codes_at(min(c, chunks - 1));
 #pragma unroll
-        for (int r = 0; r < 4; ++r) to[r] = *(const v4u*)(p + (at16 + step(r) * 16));
+        for (int r = 0; r < 4; ++r) to[r] = load_codes<ONCE>(p + (at16 + step(r) * 16));
     };
     auto load_scales = [&](int q) {
         q = min(q, quads - 1);
@@ -508,20 +517,21 @@ static unsigned plan(LogitsArgs& a, int rows, int states) {
     csv_set_error("V=%d rows x B=%d hidden states are too many blocks", a.V, a.B);
     return 0;
 }
-template <bool MX4, int NT, int RT, int S>
+template <bool MX4, int NT, int RT, int S, bool ONCE>
 static int launch_product(LogitsArgs a, int out_type, hipStream_t st) {
     const unsigned n = plan(a, 64 * RT, 16 * NT);
     if (!n) return CSV_ESHAPE;
-    if (out_type == CSV_F32) product_kernel<MX4, NT, RT, S, float><<<n, 256, 0, st>>>(a);
-    else product_kernel<MX4, NT, RT, S, uint16_t><<<n, 256, 0, st>>>(a);
+    if (out_type == CSV_F32) product_kernel<MX4, NT, RT, S, ONCE, float><<<n, 256, 0, st>>>(a);
+    else product_kernel<MX4, NT, RT, S, ONCE, uint16_t><<<n, 256, 0, st>>>(a);
     CSV_LAUNCH_CHECK("product_kernel");
     return CSV_OK;
 }
+template <bool ONCE>
 static int launch_many(LogitsArgs a, int out_type, hipStream_t st) {
     const unsigned n = plan(a, 256, 128);
     if (!n) return CSV_ESHAPE;
-    if (out_type == CSV_F32) many_kernel<float><<<n, 256, 0, st>>>(a);
-    else many_kernel<uint16_t><<<n, 256, 0, st>>>(a);
+    if (out_type == CSV_F32) many_kernel<ONCE, float><<<n, 256, 0, st>>>(a);
+    else many_kernel<ONCE, uint16_t><<<n, 256, 0, st>>>(a);
     CSV_LAUNCH_CHECK("many_kernel");
     return CSV_OK;
 }
@@ -668,15 +678,17 @@ extern "C" int csv_mx4_logits(const csv_mx4_head* x, const uint16_t* d_h, int B,
     const int64_t full = ((int64_t)x->V + 255) / 256;             // blocks of four waves of 64 rows
     const int64_t fill = 384;
     if (act == CSV_ACT_BF16) {
-        if (B <= 16) return full >= fill ? launch_product<false, 1, 4, 2>(a, out_type, st) : launch_product<false, 1, 2, 4>(a, out_type, st);
-        if (B <= 32) return full >= fill ? launch_product<false, 2, 4, 2>(a, out_type, st) : launch_product<false, 2, 2, 2>(a, out_type, st);
+        if (B <= 16) return full >= fill ? launch_product<false, 1, 4, 2, true>(a, out_type, st) : launch_product<false, 1, 2, 4, true>(a, out_type, st);
+        if (B <= 32) return full >= fill ? launch_product<false, 2, 4, 2, true>(a, out_type, st) : launch_product<false, 2, 2, 2, true>(a, out_type, st);
         // where groups of 64 make too few blocks, groups of 32 read W more often, from cache: 60 hidden states, 50000 x 4096, 36.9 against
         // 44.1; 400, 128256 x 4096, 392 against 367.  Groups of 128 win nothing: widening W is hidden behind the products already
-        return full * ((B + 63) / 64) >= fill ? launch_product<false, 4, 4, 1>(a, out_type, st) : launch_product<false, 2, 4, 2>(a, out_type, st);
+        if (full * ((B + 63) / 64) < fill) return launch_product<false, 2, 4, 2, false>(a, out_type, st);
+        return B <= 64 ? launch_product<false, 4, 4, 1, true>(a, out_type, st) : launch_product<false, 4, 4, 1, false>(a, out_type, st);
     }
-    if (B <= 16) return full >= fill ? launch_product<true, 1, 4, 2>(a, out_type, st) : launch_product<true, 1, 2, 4>(a, out_type, st);
-    if (B <= 32) return launch_product<true, 2, 2, 4>(a, out_type, st);
-    if (B <= 64) return full >= fill ? launch_product<true, 4, 4, 1>(a, out_type, st) : launch_product<true, 4, 2, 2>(a, out_type, st);
+    if (B <= 16) return full >= fill ? launch_product<true, 1, 4, 2, true>(a, out_type, st) : launch_product<true, 1, 2, 4, true>(a, out_type, st);
+    if (B <= 32) return launch_product<true, 2, 2, 4, true>(a, out_type, st);
+    if (B <= 64) return full >= fill ? launch_product<true, 4, 4, 1, true>(a, out_type, st) : launch_product<true, 4, 2, 2, true>(a, out_type, st);
     // 100 hidden states: 24000 x 4096, 28.8 against 23.9 in groups of 64; 60000 x 2048, 22.7 against 26.8
-    return full * ((B + 127) / 128) >= fill / 2 ? launch_many(a, out_type, st) : launch_product<true, 4, 2, 2>(a, out_type, st);
+    if (full * ((B + 127) / 128) < fill / 2) return launch_product<true, 4, 2, 2, false>(a, out_type, st);
+    return B <= 128 ? launch_many<true>(a, out_type, st) : launch_many<false>(a, out_type, st);
 }

@@ -95,29 +95,29 @@ __global__ __launch_bounds__(256) void quantize_kernel(const T* __restrict__ x, 
     }
 }
 
-// values leave past the caches: four times what came in, and read by another kernel at the earliest
-__device__ __forceinline__ void store8(float* p, const float* v) {
-    __builtin_nontemporal_store(v4f{v[0], v[1], v[2], v[3]}, (v4f*)p);
-    __builtin_nontemporal_store(v4f{v[4], v[5], v[6], v[7]}, (v4f*)p + 1);
-}
-// the values have two significant bits: the high half of the float32 pattern is the bfloat16
-__device__ __forceinline__ void store8(uint16_t* p, const float* v) {
-    uint32_t w[4];
-    for (int j = 0; j < 4; ++j) w[j] = (__float_as_uint(v[2 * j]) >> 16) | (__float_as_uint(v[2 * j + 1]) & 0xffff0000u);
-    __builtin_nontemporal_store(v4u{w[0], w[1], w[2], w[3]}, (v4u*)p);
-}
+// One wave: 512 elements of a row, 16 bytes of values per lane and store, side by side.  They leave past the caches: four times what came in, and
+// read by another kernel at the earliest (128256 x 4096 to bf16 236 -> 225 us).
 template <typename T>
 __global__ __launch_bounds__(256) void dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int rows, int d, int chunks,
                                                           T* __restrict__ x, int64_t ld) {
-    const int lane = threadIdx.x & 63, e0 = blockIdx.x * 512 + lane * 8, dp = chunks * CHUNK;
-    if (e0 >= d) return;
+    constexpr int E = 16 / sizeof(T);
+    const int lane = threadIdx.x & 63, dp = chunks * CHUNK;
     for (int row = blockIdx.y * 4 + (threadIdx.x >> 6); row < rows; row += 4 * gridDim.y) {
-        const uint32_t c = *(const uint32_t*)(codes + (int64_t)row * (dp >> 1) + (e0 >> 1));
-        const float s = __uint_as_float((uint32_t)scales[(int64_t)row * (dp >> 5) + (e0 >> 5)] << 23);   // exponent field 0: 2^-127; 255: NaN
-        const v2f a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 1),
-                  e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 2), f = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 3);
-        const float v[8] = {a[0], a[1], b[0], b[1], e[0], e[1], f[0], f[1]};
-        store8(x + (int64_t)row * ld + e0, v);
+#pragma unroll
+        for (int e0 = blockIdx.x * 512 + lane * E, n = 0; n < 512 / (64 * E); ++n, e0 += 64 * E) {
+            if (e0 >= d) continue;
+            const uint8_t* from = codes + (int64_t)row * (dp >> 1) + (e0 >> 1);
+            const float s = __uint_as_float((uint32_t)scales[(int64_t)row * (dp >> 5) + (e0 >> 5)] << 23);   // exponent field 0: 2^-127; 255: NaN
+            const uint32_t c = E == 8 ? *(const uint32_t*)from : *(const uint16_t*)from;
+            const v2f a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 1);
+            if constexpr (E == 4) __builtin_nontemporal_store(v4f{a[0], a[1], b[0], b[1]}, (v4f*)(x + (int64_t)row * ld + e0));
+            else {
+                // the values have two significant bits: the high half of the float32 pattern is the bfloat16
+                const v2f e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 2), f = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 3);
+                auto both = [](const v2f& v) { return (__float_as_uint(v[0]) >> 16) | (__float_as_uint(v[1]) & 0xffff0000u); };
+                __builtin_nontemporal_store(v4u{both(a), both(b), both(e), both(f)}, (v4u*)(x + (int64_t)row * ld + e0));
+            }
+        }
     }
 }
 
@@ -672,16 +672,16 @@ extern "C" int csv_mx4_logits(const csv_mx4_head* x, const uint16_t* d_h, int B,
         a.hs = (const uint32_t*)hs;
     }
     // Waves that take 64 rows each read h least often, waves of 32 rows make more blocks: below three blocks for two compute units
-    // the units that have none, or two, cost more.  Microseconds, 16 / 32 / 64 rows a wave:
-    // bf16, 14 hidden states, 80000 x 4096: 36.2 / 36.5 / 39.8, 16 of them, 128256 x 4096: 60.6 / 55.7 / 51.1;  30, 80000 x 4096: - / 40.6 / 43.9,
-    // 32, 256000 x 4608: - / 135 / 131;  4 bits, 64, 128256 x 8192: - / 119 / 113, 60, 80000 x 4096: - / 43.0 / 45.7.
+    // the units that have none, or two, cost more.  Microseconds, 32 / 64 rows a wave, from d = 4096: bf16, 14 hidden states, V = 80000
+    // 32.5 / 36.3, 100000 42.1 / 39.3, 128256 48.1 / 44.9;  30 of them, 80000 38.3 / 41.0, 100000 48.9 / 43.2;  4 bits, 60, 80000 39.3 / 43.2,
+    // 128256 55.9 / 52.7.  (16 rows: 32.9 and 54.5 for 14 at 80000 and 128256.)
     const int64_t full = ((int64_t)x->V + 255) / 256;             // blocks of four waves of 64 rows
     const int64_t fill = 384;
     if (act == CSV_ACT_BF16) {
         if (B <= 16) return full >= fill ? launch_product<false, 1, 4, 2, true>(a, out_type, st) : launch_product<false, 1, 2, 4, true>(a, out_type, st);
         if (B <= 32) return full >= fill ? launch_product<false, 2, 4, 2, true>(a, out_type, st) : launch_product<false, 2, 2, 2, true>(a, out_type, st);
-        // where groups of 64 make too few blocks, groups of 32 read W more often, from cache: 60 hidden states, 50000 x 4096, 36.9 against
-        // 44.1; 400, 128256 x 4096, 392 against 367.  Groups of 128 win nothing: widening W is hidden behind the products already
+        // where groups of 64 make too few blocks, groups of 32 read W more often, from cache: 60 hidden states, 50000 x 4096, 36.2 against
+        // 42.7, 128256 x 4096, 82.4 against 69.8.  Groups of 128 win nothing (817 against 832 for 1024): widening W is hidden behind the products
         if (full * ((B + 63) / 64) < fill) return launch_product<false, 2, 4, 2, false>(a, out_type, st);
         return B <= 64 ? launch_product<false, 4, 4, 1, true>(a, out_type, st) : launch_product<false, 4, 4, 1, false>(a, out_type, st);
     }

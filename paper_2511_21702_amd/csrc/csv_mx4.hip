@@ -492,7 +492,8 @@ __global__ __launch_bounds__(256, 2) void many_kernel(LogitsArgs a) {
         if (left > 3) products(std::integral_constant<int, 3>(), last, w[3]);
     }
 
-    // lane l holds rows 8 i + 4 (l / 32) .. + 3 of hidden state l % 32 of a block of 32 x 32
+    // lane l holds rows 8 i + 4 (l / 32) .. + 3 of hidden state l % 32 of a block of 32 x 32; h of a stage that was not needed may still be on its way
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     float* buf = (float*)lds + wave * 32 * OW;
 #pragma unroll

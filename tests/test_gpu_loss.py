@@ -186,6 +186,33 @@ def test_masked_rows_and_values_that_are_not_finite(dtype, V, N):
     assert bool(torch.isnan(loss)) and bool(torch.isnan(grad[4].float()).all())
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N,V", [(6, 5003), (6, 90001), (300, 5003)])
+@pytest.mark.parametrize("offset,mask,c", [(0.0, -1e4, 1.0), (0.0, -1e9, 1.3), (3e5, -1e30, 1.0), (-3e5, -1e9, 0.7), (1e6, -1e6, 1.0), (-2e8, -1e30, 1.0), (1e30, 0.0, 1e-29)])
+def test_logits_far_from_zero_and_masks_by_addition(dtype, N, V, offset, mask, c):
+    """Most of every row far below, by a number that is added, and rows whose largest logit is far from zero on either side."""
+    csv = _csv()
+    log(f"far rows N={N} V={V} {dtype} offset={offset} mask={mask}")
+    c = float(np.float32(c))
+    gen = torch.Generator().manual_seed(7)
+    x = torch.randn(N, V, generator=gen) * (2 if abs(offset) < 1e29 else 1e29) + offset
+    x[:, V // 3:] += mask
+    t = torch.randint(0, V // 3, (N,), generator=gen)
+    x = _place(x, dtype, gap=3, shift=1)
+    t = t.to(torch.int32).cuda()
+    logp, stats = csv.csv_token_logprobs(x, t, c)
+    x64, t64 = x.cpu().double().numpy(), t.cpu().numpy()
+    m, s, want, p = O.rows_logp(x64, t64, c)
+    tol, rel = O.logp_tolerance(x64, m, p, c, want)
+    assert (np.abs(logp.cpu().double().numpy() - want) <= tol).all()
+    st = stats.cpu().double().numpy()
+    assert (st[:, 0] == m).all() and (np.abs(st[:, 1] - s) <= s * (rel + O.U24)).all()
+    g = torch.linspace(-1, 1, N)
+    grad = csv.csv_token_logprobs_backward(x, t, stats, g.cuda(), c).cpu().double().numpy()
+    _grad_close(grad, p, s, t64, g.double().numpy(), c, rel, x64, m, dtype)
+    _policy_check(csv, x, t, c, 0.2, 0.28, 0.05, N + V, dtype)
+
+
 def test_no_rows():
     csv = _csv()
     e = torch.empty(0, device="cuda")

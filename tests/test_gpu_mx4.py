@@ -158,6 +158,20 @@ def test_logits_of_long_rows_and_many_rows(V, d, B, act):
     head.free()
 
 
+@pytest.mark.parametrize("d", [64, 128, 264, 384, 512, 520, 768, 896, 1032, 1160])
+@pytest.mark.parametrize("B", [66, 130])
+def test_logits_of_many_hidden_states_at_every_number_of_steps(d, B):
+    """Rows of one to ten steps of 128 elements, in tiles for many rows and many hidden states, one group of them and two."""
+    csv = _csv()
+    V = 50003
+    log(f"logits V={V} d={d} B={B}")
+    head, W, b = _head(V, d, d)
+    h = torch.randn(B, d, generator=torch.Generator().manual_seed(B)).to(BF16)
+    for out_type in (F32, BF16):
+        _check(head, W, b, h, 1, out_type, csv.csv_mx4_logits(head, h.cuda(), act=1, dtype=out_type))
+    head.free()
+
+
 @pytest.mark.parametrize("act", [0, 1])
 @pytest.mark.parametrize("B", [3, 80])
 def test_values_that_are_not_finite_stay_in_their_row_and_column(act, B):

@@ -410,10 +410,11 @@ static int check_scratch(size_t need, const void* p, size_t have) {
 
 // Where the rows alone leave compute units without work, or with too little of it to keep the memory busy, a row is cut into parts.  Below
 // FEW_ROWS two launches over parts win, though they read the logits twice, from FEW_ROWS on one block per row does (policy loss, us,
-// parts / row: 64 rows of 128256 bf16 14.5 / 25, 250 of them 41 / 32, 1000 rows of 100000 float32 213 / 182).  Without a gradient one block
-// per row stays ahead up to LONG_ROW logits, where the second launch costs more than the parts save.
-#define FEW_ROWS 192
-#define LONG_ROW 65536
+// parts / row: 64 rows of 128256 bf16 14.5 / 20.7, 100 of them 19.0 / 21.4, 128 23.0 / 21.9, 190 30.2 / 25.7).  Without a gradient one block per
+// row is one launch, and stays ahead up to longer rows the more rows there are (parts / row: 1 row of 32000 float32 6.1 / 4.3, of 128256
+// 6.6 / 8.1, 32 of 128256 8.5 / 9.6, 64 of 128256 11.2 / 9.9, 64 of 256000 bf16 12.0 / 14.5).
+#define FEW_ROWS 112
+#define LONG_ROW(N) (65000 + 1500 * (N))
 #define PART_BLOCKS 2048            // blocks of 256 threads that are resident together
 #define GRAD_BLOCKS 16384           // gradients from given statistics have nothing to join: short blocks (us for 509 x 151669 bf16, 2048 x
                                     // 128256 float32: 64, 412 with 4096 blocks, 54, 391 with 16384)
@@ -429,7 +430,7 @@ static int scratch_bytes(int N, int V, bool parts, size_t* bytes) {
     *bytes = (size_t)N * sizeof(double) + (parts && N > 0 ? (size_t)N * (sizeof(float2) * parts_of(N, V, PART_BLOCKS) + 8) + 8 : 0);
     return CSV_OK;
 }
-static inline bool logprobs_by_parts(int N, int V) { return N < FEW_ROWS && V > LONG_ROW; }
+static inline bool logprobs_by_parts(int N, int V) { return N < FEW_ROWS && V > LONG_ROW(N); }
 
 extern "C" int csv_policy_loss_scratch(int N, int V, size_t* bytes) { return scratch_bytes(N, V, N < FEW_ROWS, bytes); }
 

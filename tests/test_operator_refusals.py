@@ -69,6 +69,8 @@ def test_loss_refused(csv):
         assert f(0, 70000, C.byref(n)) == 0 and n.value == 0
     assert csv.lib.csv_policy_loss_scratch(3, 100, C.byref(n)) == 0 and n.value >= 24
     assert csv.lib.csv_token_logprobs_scratch(3, 100, C.byref(n)) == 0 and n.value == 0
+    assert csv.lib.csv_policy_loss_scratch(2 ** 31 - 1, 100, C.byref(n)) == 0 and n.value >= 8 * (2 ** 31 - 1)
+    assert csv.lib.csv_token_logprobs_scratch(2 ** 31 - 1, 2 ** 31 - 1, C.byref(n)) == 0 and n.value == 0
     big = 1 << 40
 
     def fwd(x=P, ty=0, ld=70000, N=3, V=70000, t=P, c=1.0, logp=P, stats=P, scr=P, size=big):

@@ -226,7 +226,7 @@ __device__ __forceinline__ double policy_term(const RowArgs& a, int i, double lo
     const double A = a.adv[i], w = a.weights[i], r = exp(logp - (double)a.old_logp[i]);
     const double lo = 1.0 - (double)a.clip_low, hi = 1.0 + (double)a.clip_high, whole = r * A, cut = fmin(fmax(r, lo), hi) * A;
     double term = cut < whole ? -cut : -whole;
-    double d = (A >= 0.0 ? r <= hi : r >= lo) ? -A * r : 0.0;
+    double d = (A >= 0.0 ? r > hi : r < lo) ? 0.0 * A : -whole;      // a NaN of the inputs is one of the gradient too
     if (a.beta > 0.f) {
         const double k = (double)a.ref_logp[i] - logp, em = expm1(k);
         term += (double)a.beta * (em - k);

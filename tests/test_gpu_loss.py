@@ -224,6 +224,23 @@ def test_no_rows():
     csv.csv_token_logprobs_backward(torch.empty(0, 50, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda"), stats, e)
 
 
+@pytest.mark.parametrize("N", [5, 200])
+def test_inputs_of_a_row_that_are_not_numbers_show_in_its_gradient_alone(N):
+    csv = _csv()
+    V = 3001
+    x, t = _rows(N, V, F32, 4)
+    base, _ = csv.csv_token_logprobs(x, t)
+    nan = float("nan")
+    for k in range(4):                                   # old_logp, ref_logp, advantages, weights
+        v = [base.clone(), base.clone(), torch.ones(N, device="cuda"), torch.full((N,), 1.0 / N, device="cuda")]
+        v[k][2] = nan
+        for ratio in (0.0, 1.0, -1.0):                   # on both sides of the clip
+            old = v[0] - ratio
+            loss, logp, grad = csv.csv_policy_loss(x, t, old, v[1], v[2], v[3], beta=0.1)
+            assert bool(torch.isnan(loss)) and bool(torch.isnan(grad[2]).all()) and bool(torch.isfinite(logp).all())
+            assert bool(torch.isfinite(grad[[i for i in range(N) if i != 2]]).all())
+
+
 def test_all_rows_left_out():
     csv = _csv()
     x = torch.full((5, 4099), float("nan"), device="cuda")

@@ -48,21 +48,19 @@ __host__ __device__ static inline int64_t codes_at(int c) { return (int64_t)c * 
 struct Elems8 {
     float v[8];
 };
-__device__ __forceinline__ Elems8 load8(const uint16_t* p) {
-    const uint4 u = *(const uint4*)p;
+__device__ __forceinline__ Elems8 widen8(const v4u& u) {
     return {{bf16_lo(u.x), bf16_hi(u.x), bf16_lo(u.y), bf16_hi(u.y), bf16_lo(u.z), bf16_hi(u.z), bf16_lo(u.w), bf16_hi(u.w)}};
 }
+__device__ __forceinline__ Elems8 load8(const uint16_t* p) { return widen8(*(const v4u*)p); }
 __device__ __forceinline__ Elems8 load8(const float* p) {
     const float4 a = ((const float4*)p)[0], b = ((const float4*)p)[1];
     return {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
 }
-__device__ __forceinline__ uint32_t round8(const Elems8& x, uint32_t& scale) {
-    uint32_t m = 0;
-    for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(x.v[j]) & 0x7fffffffu);
-    m = max(m, (uint32_t)dpp_move<0xB1, 0xf>((int)m, (int)m));   // quad_perm [1,0,3,2]
-    m = max(m, (uint32_t)dpp_move<0x4E, 0xf>((int)m, (int)m));   // quad_perm [2,3,0,1]
-    const uint32_t field = m >> 23;
-    scale = field == 255u ? 255u : field > 2u ? field - 2u : 0u;
+__device__ __forceinline__ uint32_t scale_of(uint32_t largest) {    // from the float32 pattern of the largest magnitude
+    const uint32_t field = largest >> 23;
+    return field == 255u ? 255u : field > 2u ? field - 2u : 0u;
+}
+__device__ __forceinline__ uint32_t codes8(const Elems8& x, uint32_t scale) {
     const float inv = __uint_as_float((254u - (scale == 255u ? 0u : scale)) << 23);
     uint32_t r = 0;
     r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x.v[0] * inv, x.v[1] * inv, 1.0f, 0);
@@ -70,6 +68,17 @@ __device__ __forceinline__ uint32_t round8(const Elems8& x, uint32_t& scale) {
     r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x.v[4] * inv, x.v[5] * inv, 1.0f, 2);
     r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x.v[6] * inv, x.v[7] * inv, 1.0f, 3);
     return scale == 255u ? 0u : r;
+}
+__device__ __forceinline__ uint32_t largest8(const Elems8& x, uint32_t m) {
+    for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(x.v[j]) & 0x7fffffffu);
+    return m;
+}
+__device__ __forceinline__ uint32_t round8(const Elems8& x, uint32_t& scale) {
+    uint32_t m = largest8(x, 0);
+    m = max(m, (uint32_t)dpp_move<0xB1, 0xf>((int)m, (int)m));   // quad_perm [1,0,3,2]
+    m = max(m, (uint32_t)dpp_move<0x4E, 0xf>((int)m, (int)m));   // quad_perm [2,3,0,1]
+    scale = scale_of(m);
+    return codes8(x, scale);
 }
 
 // One wave: 512 elements of a row (blockIdx.x), rows blockIdx.y * 4 + wave and every 4 * gridDim.y rows further.  TILES: codes and scales go
@@ -228,21 +237,27 @@ __device__ __forceinline__ v4u load_codes(const uint8_t* p) {
     else return *(const v4u*)p;
 }
 
+// how the hidden states come: as they are, as 4-bit tiles, or to be rounded on the way to LDS
+enum { H_BF16, H_TILES, H_ROUNDED_HERE };
+
 // Four waves, RT tiles of 16 rows each, against NT groups of 16 hidden states; K goes by in stages of S tiles of 128.
 //
 // The sum over k may run in any order that both operands share.  A tile puts element 32 (l / 16) + 8 s + j at lane l, so a 4-bit tile goes to
 // one 16x16x128 instruction as it is, and against bf16 it is widened (exactly) to four operands s = 0..3 of 16x16x32.
 // Codes of W are read once, straight into registers, a stage ahead: a register is requested again as soon as its products are issued.  The
 // stage of h lies in LDS, two buffers, and passes through registers on its way there, so that a barrier waits for no load.  bf16 h lies row by
-// row with the 16-byte pieces of row t exchanged by t % 16 (a column of pieces then spreads over all banks); 4-bit h lies as its tiles.
+// row with the 16-byte pieces of row t exchanged by t % 16 (a column of pieces then spreads over all banks); 4-bit h lies as its tiles, which few
+// hidden states become here (a thread rounds a block: cheaper than a launch, while the block waits for W).
 // Past the end of a row or of the batch the last piece or row is read again: codes of W are 0 there, and those hidden states are not stored.
-template <bool MX4, int NT, int RT, int S, bool ONCE, typename T>
+template <int H, int NT, int RT, int S, bool ONCE, typename T>
 __global__ __launch_bounds__(256, 3) void product_kernel(LogitsArgs a) {
+    constexpr bool MX4 = H != H_BF16, HERE = H == H_ROUNDED_HERE;
     constexpr int HP = NT * S * (MX4 ? 64 : 256);                 // 16-byte pieces of a stage of h
     constexpr int HT = (HP + 255) / 256;                          // of them per thread
     constexpr int OW = RT * 16 + 4;                               // floats per hidden state in a wave's part of the output buffer
     constexpr int LDS = 2 * HP > 16 * OW ? 2 * HP : 16 * OW;      // four waves' parts
     __shared__ v4u lds[LDS];
+    __shared__ uint32_t hscale[HERE ? 2 * NT * 64 : 1];           // of h that is rounded here, a byte per step of the stage
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, col = lane & 15;
     // blocks of one die (every eighth) take the groups of hidden states of one block of rows after each other: W comes from that die's cache
     const int j = blockIdx.x >> 3, group = j % a.groups, block = (j / a.groups) * 8 + (blockIdx.x & 7);
@@ -252,9 +267,9 @@ __global__ __launch_bounds__(256, 3) void product_kernel(LogitsArgs a) {
     const uint8_t* band = a.bands + (tile0 >> 2) * band_bytes(chunks);
     const uint8_t *wc = band + (tile0 & 3) * 1024 + lane * 16, *ws = band + (tile0 & 3) * 256 + lane * 4;
     const int64_t htile0 = (int64_t)group * NT;
-    const uint32_t* hs = MX4 ? a.hs + htile0 * quads * 64 + lane : nullptr;
+    const uint32_t* hs = MX4 && !HERE ? a.hs + htile0 * quads * 64 + lane : nullptr;
 
-    v4u w[S][RT], hr[HT];
+    v4u w[S][RT], hr[HERE ? 4 * HT : HT];
     uint32_t sw[RT], sh[MX4 ? NT : 1], sw_next[RT], sh_next[MX4 ? NT : 1];
     auto load_w = [&](int c, v4u (&to)[RT]) {
         const int cc = min(c, chunks - 1);
@@ -265,7 +280,7 @@ __global__ __launch_bounds__(256, 3) void product_kernel(LogitsArgs a) {
         const int q = min(c0, chunks - 1) >> 2;
 #pragma unroll
         for (int r = 0; r < RT; ++r) sw_next[r] = *(const uint32_t*)(ws + scales_at(q) + r * 256);
-        if (MX4)
+        if (MX4 && !HERE)
 #pragma unroll
             for (int n = 0; n < NT; ++n) sh_next[n] = hs[((int64_t)n * quads + q) * 64];
     };
@@ -274,7 +289,12 @@ __global__ __launch_bounds__(256, 3) void product_kernel(LogitsArgs a) {
         for (int i = 0; i < HT; ++i) {
             const int p = tid + i * 256;
             if (HP % 256 != 0 && p >= HP) continue;
-            if (MX4) {
+            if constexpr (HERE) {                                 // block p / 16 % 4 of a step of hidden state p % 16: 64 bytes
+                const int c = p / (NT * 64), n = p / 64 % NT, e = (c0 + c) * CHUNK + (p >> 4 & 3) * BLK;
+                const int64_t b = min((int)(htile0 * 16) + n * 16 + (p & 15), a.B - 1);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) hr[4 * i + k] = *(const v4u*)(a.h + b * a.d + min(e + 8 * k, a.d - 8));
+            } else if constexpr (MX4) {
                 const int c = p / (NT * 64), n = p / 64 % NT;
                 hr[i] = ((const v4u*)a.hc)[((htile0 + n) * chunks + min(c0 + c, chunks - 1)) * 64 + (p & 63)];
             } else {
@@ -284,11 +304,27 @@ __global__ __launch_bounds__(256, 3) void product_kernel(LogitsArgs a) {
             }
         }
     };
-    auto store_h = [&](int buf) {
+    auto store_h = [&](int buf, int c0) {
 #pragma unroll
         for (int i = 0; i < HT; ++i) {
             const int p = tid + i * 256;
             if (HP % 256 != 0 && p >= HP) continue;
+            if constexpr (HERE) {
+                const int c = p / (NT * 64), left = a.d - (c0 + c) * CHUNK - (p >> 4 & 3) * BLK;      // elements of the row from this block on
+                uint32_t m = 0;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (left <= 8 * k) hr[4 * i + k] = v4u{0, 0, 0, 0};
+                    m = largest8(widen8(hr[4 * i + k]), m);
+                }
+                const uint32_t scale = scale_of(m);
+                v4u codes;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) codes[k] = codes8(widen8(hr[4 * i + k]), scale);
+                lds[buf * HP + p] = codes;
+                ((uint8_t*)hscale)[(buf * NT * 64 + p % (NT * 64)) * 4 + c] = (uint8_t)scale;
+                continue;
+            }
             lds[buf * HP + (MX4 ? p : p ^ (p >> 4 & 15))] = hr[i];
         }
     };
@@ -325,9 +361,14 @@ __global__ __launch_bounds__(256, 3) void product_kernel(LogitsArgs a) {
     auto take_scales = [&](int c0) {
 #pragma unroll
         for (int r = 0; r < RT; ++r) sw[r] = sw_next[r] >> (8 * (c0 & 3));
-        if (MX4)
+        if (MX4 && !HERE)
 #pragma unroll
             for (int n = 0; n < NT; ++n) sh[n] = sh_next[n] >> (8 * (c0 & 3));
+    };
+    auto read_hscales = [&](int buf) {                            // after the barrier
+        if (HERE)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) sh[n] = hscale[(buf * NT + n) * 64 + lane];
     };
 
     load_h(0);
@@ -335,11 +376,12 @@ __global__ __launch_bounds__(256, 3) void product_kernel(LogitsArgs a) {
 #pragma unroll
     for (int c = 0; c < S; ++c) load_w(c, w[c]);
     for (int st = 0; st < stages - 1; ++st) {
-        store_h(st & 1);
+        store_h(st & 1, st * S);
         take_scales(st * S);
         load_h((st + 1) * S);
         load_scales((st + 1) * S);
         lds_barrier();
+        read_hscales(st & 1);
 #pragma unroll
         for (int c = 0; c < S; ++c) {
             products(st & 1, c, w[c]);
@@ -348,9 +390,10 @@ __global__ __launch_bounds__(256, 3) void product_kernel(LogitsArgs a) {
         }
     }
     const int last = stages - 1;                                  // the last stage asks for nothing more
-    store_h(last & 1);
+    store_h(last & 1, last * S);
     take_scales(last * S);
     lds_barrier();
+    read_hscales(last & 1);
 #pragma unroll
     for (int c = 0; c < S; ++c)
         if (last * S + c < chunks) products(last & 1, c, w[c]);
@@ -518,12 +561,12 @@ static unsigned plan(LogitsArgs& a, int rows, int states) {
     csv_set_error("V=%d rows x B=%d hidden states are too many blocks", a.V, a.B);
     return 0;
 }
-template <bool MX4, int NT, int RT, int S, bool ONCE>
+template <int H, int NT, int RT, int S, bool ONCE>
 static int launch_product(LogitsArgs a, int out_type, hipStream_t st) {
     const unsigned n = plan(a, 64 * RT, 16 * NT);
     if (!n) return CSV_ESHAPE;
-    if (out_type == CSV_F32) product_kernel<MX4, NT, RT, S, ONCE, float><<<n, 256, 0, st>>>(a);
-    else product_kernel<MX4, NT, RT, S, ONCE, uint16_t><<<n, 256, 0, st>>>(a);
+    if (out_type == CSV_F32) product_kernel<H, NT, RT, S, ONCE, float><<<n, 256, 0, st>>>(a);
+    else product_kernel<H, NT, RT, S, ONCE, uint16_t><<<n, 256, 0, st>>>(a);
     CSV_LAUNCH_CHECK("product_kernel");
     return CSV_OK;
 }
@@ -630,9 +673,10 @@ static int check_logits(const csv_mx4_head* x, int B, int act) {
     if (act != CSV_ACT_BF16 && act != CSV_ACT_MX4) { csv_set_error("bad act=%d", act); return CSV_EINVAL; }
     return CSV_OK;
 }
+#define ROUNDED_HERE 16             // hidden states that the product rounds to 4 bits itself
 // tiles of the 4-bit copy of h: a whole number of what a block of the product takes together
 static inline int64_t tiles_of(int B) {
-    const int64_t nt = B <= 16 ? 1 : B <= 32 ? 2 : B <= 64 ? 4 : 8;
+    const int64_t nt = B <= 32 ? 2 : B <= 64 ? 4 : 8;
     return ((int64_t)B + 16 * nt - 1) / (16 * nt) * nt;
 }
 
@@ -640,7 +684,7 @@ extern "C" int csv_mx4_logits_scratch(const csv_mx4_head* x, int B, int act, siz
     const int rc = check_logits(x, B, act);
     if (rc) return rc;
     if (!bytes) { csv_set_error("null bytes"); return CSV_EINVAL; }
-    *bytes = act == CSV_ACT_BF16 ? 0 : (size_t)tiles_of(B) * ((size_t)x->chunks * 1024 + (size_t)((x->chunks + 3) / 4) * 256);
+    *bytes = act == CSV_ACT_BF16 || B <= ROUNDED_HERE ? 0 : (size_t)tiles_of(B) * ((size_t)x->chunks * 1024 + (size_t)((x->chunks + 3) / 4) * 256);
     return CSV_OK;
 }
 
@@ -664,7 +708,7 @@ extern "C" int csv_mx4_logits(const csv_mx4_head* x, const uint16_t* d_h, int B,
     a.bands = x->bands; a.bias = x->bias; a.V = x->V; a.d = x->d; a.chunks = x->chunks; a.B = B; a.h = d_h; a.out = d_logits;
     a.wide = ((uintptr_t)d_logits & 15) == 0 && x->V % (out_type == CSV_F32 ? 4 : 8) == 0;
     const int64_t tt = tiles_of(B);
-    if (act == CSV_ACT_MX4) {
+    if (need) {
         uint8_t* hc = (uint8_t*)d_scratch;
         uint8_t* hs = hc + (size_t)tt * x->chunks * 1024;
         quantize_kernel<uint16_t, true><<<rows_grid((int)(tt * 16), x->chunks), 256, 0, st>>>(d_h, x->d, B, (int)(tt * 16), x->d, x->chunks, hc, hs);
@@ -679,17 +723,17 @@ extern "C" int csv_mx4_logits(const csv_mx4_head* x, const uint16_t* d_h, int B,
     const int64_t full = ((int64_t)x->V + 255) / 256;             // blocks of four waves of 64 rows
     const int64_t fill = 384;
     if (act == CSV_ACT_BF16) {
-        if (B <= 16) return full >= fill ? launch_product<false, 1, 4, 2, true>(a, out_type, st) : launch_product<false, 1, 2, 4, true>(a, out_type, st);
-        if (B <= 32) return full >= fill ? launch_product<false, 2, 4, 2, true>(a, out_type, st) : launch_product<false, 2, 2, 2, true>(a, out_type, st);
+        if (B <= 16) return full >= fill ? launch_product<H_BF16, 1, 4, 2, true>(a, out_type, st) : launch_product<H_BF16, 1, 2, 4, true>(a, out_type, st);
+        if (B <= 32) return full >= fill ? launch_product<H_BF16, 2, 4, 2, true>(a, out_type, st) : launch_product<H_BF16, 2, 2, 2, true>(a, out_type, st);
         // where groups of 64 make too few blocks, groups of 32 read W more often, from cache: 60 hidden states, 50000 x 4096, 36.2 against
         // 42.7, 128256 x 4096, 82.4 against 69.8.  Groups of 128 win nothing (817 against 832 for 1024): widening W is hidden behind the products
-        if (full * ((B + 63) / 64) < fill) return launch_product<false, 2, 4, 2, false>(a, out_type, st);
-        return B <= 64 ? launch_product<false, 4, 4, 1, true>(a, out_type, st) : launch_product<false, 4, 4, 1, false>(a, out_type, st);
+        if (full * ((B + 63) / 64) < fill) return launch_product<H_BF16, 2, 4, 2, false>(a, out_type, st);
+        return B <= 64 ? launch_product<H_BF16, 4, 4, 1, true>(a, out_type, st) : launch_product<H_BF16, 4, 4, 1, false>(a, out_type, st);
     }
-    if (B <= 16) return full >= fill ? launch_product<true, 1, 4, 2, true>(a, out_type, st) : launch_product<true, 1, 2, 4, true>(a, out_type, st);
-    if (B <= 32) return launch_product<true, 2, 2, 4, true>(a, out_type, st);
-    if (B <= 64) return full >= fill ? launch_product<true, 4, 4, 1, true>(a, out_type, st) : launch_product<true, 4, 2, 2, true>(a, out_type, st);
+    if (B <= ROUNDED_HERE) return full >= fill ? launch_product<H_ROUNDED_HERE, 1, 4, 2, true>(a, out_type, st) : launch_product<H_ROUNDED_HERE, 1, 2, 4, true>(a, out_type, st);
+    if (B <= 32) return launch_product<H_TILES, 2, 2, 4, true>(a, out_type, st);
+    if (B <= 64) return full >= fill ? launch_product<H_TILES, 4, 4, 1, true>(a, out_type, st) : launch_product<H_TILES, 4, 2, 2, true>(a, out_type, st);
     // 100 hidden states: 24000 x 4096, 28.8 against 23.9 in groups of 64; 60000 x 2048, 22.7 against 26.8
-    if (full * ((B + 127) / 128) < fill / 2) return launch_product<true, 4, 2, 2, false>(a, out_type, st);
+    if (full * ((B + 127) / 128) < fill / 2) return launch_product<H_TILES, 4, 2, 2, false>(a, out_type, st);
     return B <= 128 ? launch_many<true>(a, out_type, st) : launch_many<false>(a, out_type, st);
 }

@@ -158,6 +158,24 @@ def test_logits_of_long_rows_and_many_rows(V, d, B, act):
     head.free()
 
 
+@pytest.mark.parametrize("act", [0, 1])
+@pytest.mark.parametrize("V,d", [(3001, 1032), (50003, 520), (98400, 264)])
+def test_bits_of_a_row_do_not_depend_on_the_batch(V, d, act):
+    """One order of sums, whatever the tiles; scales far apart, so that sums round."""
+    csv = _csv()
+    gen = torch.Generator().manual_seed(d)
+    dp = O.padded(d)
+    codes = torch.randint(0, 256, (V, dp // 2), generator=gen, dtype=torch.uint8)
+    scales = torch.randint(105, 135, (V, dp // 32), generator=gen, dtype=torch.uint8)
+    head = csv.csv_mx4_head(codes.cuda(), scales.cuda(), None, d)
+    h = (torch.randn(130, d, generator=gen) * torch.exp(3 * torch.randn(130, d, generator=gen))).to(BF16).cuda()
+    whole = csv.csv_mx4_logits(head, h, act=act)
+    for B in (1, 7, 16, 17, 32, 33, 64, 65, 100):
+        log(f"V={V} d={d} B={B}")
+        assert torch.equal(csv.csv_mx4_logits(head, h[:B], act=act), whole[:B])
+    head.free()
+
+
 @pytest.mark.parametrize("d", [64, 128, 264, 384, 512, 520, 768, 896, 1032, 1160])
 @pytest.mark.parametrize("B", [66, 130])
 def test_logits_of_many_hidden_states_at_every_number_of_steps(d, B):
@@ -273,7 +291,7 @@ def test_refusals_on_the_device():
         csv.csv_mx4_logits(head, h, act=2)
     assert e.value.code == -1
     with pytest.raises(csv.CsvError) as e:
-        csv.csv_mx4_logits(head, h, act=csv.ACT_MX4, scratch=torch.empty(16, dtype=torch.uint8, device="cuda"))
+        csv.csv_mx4_logits(head, torch.zeros(20, 64, dtype=BF16, device="cuda"), act=csv.ACT_MX4, scratch=torch.empty(16, dtype=torch.uint8, device="cuda"))
     assert e.value.code == -4 and "scratch" in str(e.value)
     with pytest.raises(csv.CsvError):
         csv.csv_mx4_logits(head, torch.zeros(csv.MX4_MAX_BATCH + 1, 64, dtype=BF16, device="cuda"), out=torch.empty(csv.MX4_MAX_BATCH + 1, 40, device="cuda"))

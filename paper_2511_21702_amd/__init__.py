@@ -393,6 +393,7 @@ _TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.int16: BF16}     # int
 
 # The calls below are short next to a kernel of a few microseconds, so their checks are plain comparisons; the device and the raw stream
 # are asked for without building stream objects.
+_current_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
 
 def _rows(t: torch.Tensor, what: str) -> tuple:
@@ -404,7 +405,7 @@ def _rows(t: torch.Tensor, what: str) -> tuple:
     ld, step = t.stride()
     if step != 1 and cols > 1:
         raise ValueError(f"{what} must have contiguous rows")
-    if dev < 0 or dev != torch._C._cuda_getDevice():
+    if dev < 0 or dev != _current_device():
         raise ValueError(f"{what} must be on the current CUDA device")
     return ty, dev, ld if rows > 1 else cols
 
@@ -416,9 +417,16 @@ def _dense(t: torch.Tensor, what: str, dtype, shape: tuple, dev: int) -> int:
     return t.data_ptr()
 
 
+def _vector(t: torch.Tensor, what: str, dtype, n: int, dev: int) -> int:
+    """Pointer of a contiguous tensor of this type with n elements on device `dev`."""
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of {n} elements on the device of the call")
+    return t.data_ptr()
+
+
 def _device_of(t: torch.Tensor, what: str) -> int:
     dev = t.get_device()
-    if dev < 0 or dev != torch._C._cuda_getDevice():
+    if dev < 0 or dev != _current_device():
         raise ValueError(f"{what} must be on the current CUDA device")
     return dev
 
@@ -453,7 +461,7 @@ def csv_mx4_quantize(x: torch.Tensor, codes: torch.Tensor | None = None, scales:
     if scales is None:
         scales = torch.empty((rows, dp // 32), dtype=torch.uint8, device=dev)
     _check(lib.csv_mx4_quantize(x.data_ptr(), ty, ld, rows, d, _dense(codes, "codes", torch.uint8, (rows, dp // 2), dev),
-                                _dense(scales, "scales", torch.uint8, (rows, dp // 32), dev), torch._C._cuda_getCurrentRawStream(dev)))
+                                _dense(scales, "scales", torch.uint8, (rows, dp // 32), dev), _raw_stream(dev)))
     return codes, scales
 
 
@@ -469,7 +477,7 @@ def csv_mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, d: int, out: t
     if out.shape != (rows, d):
         raise ValueError(f"out must have the shape {(rows, d)}")
     _check(lib.csv_mx4_dequantize(_dense(codes, "codes", torch.uint8, (rows, dp // 2), dev), _dense(scales, "scales", torch.uint8, (rows, dp // 32), dev),
-                                  rows, d, out.data_ptr(), ty, ld, torch._C._cuda_getCurrentRawStream(dev)))
+                                  rows, d, out.data_ptr(), ty, ld, _raw_stream(dev)))
     return out
 
 
@@ -526,7 +534,7 @@ def csv_mx4_logits(head: CsvMx4Head, h: torch.Tensor, out: torch.Tensor | None =
         raise ValueError("out must be float32 or bfloat16")
     keep, ptr, size = _scratch(0 if act == ACT_BF16 else head.scratch_bytes(B, act), scratch, dev)
     _check(lib.csv_mx4_logits(head._h, h.data_ptr(), B, act, _dense(out, "out", out.dtype, (B, head.V), dev), ty, ptr, size,
-                              torch._C._cuda_getCurrentRawStream(dev)))
+                              _raw_stream(dev)))
     return out
 
 
@@ -559,9 +567,9 @@ def csv_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, inv_temperatu
     if stats is None:
         stats = torch.empty((N, 2), dtype=torch.float32, device=dev)
     keep, ptr, size = _scratch(csv_token_logprobs_scratch(N, V), scratch, dev)
-    _check(lib.csv_token_logprobs(logits.data_ptr(), ty, ld, N, V, _dense(tokens, "tokens", torch.int32, (N,), dev), inv_temperature,
-                                  _dense(logp, "logp", torch.float32, (N,), dev), _dense(stats, "stats", torch.float32, (N, 2), dev), ptr, size,
-                                  torch._C._cuda_getCurrentRawStream(dev)))
+    _check(lib.csv_token_logprobs(logits.data_ptr(), ty, ld, N, V, _vector(tokens, "tokens", torch.int32, N, dev), inv_temperature,
+                                  _vector(logp, "logp", torch.float32, N, dev), _vector(stats, "stats", torch.float32, 2 * N, dev), ptr, size,
+                                  _raw_stream(dev)))
     return logp, stats
 
 
@@ -584,9 +592,9 @@ def csv_token_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor, stat
     if grad is None:
         grad = torch.empty((N, V), dtype=logits.dtype, device=dev)
     gp, gld = _grad_of(logits, grad, ty, dev)
-    _check(lib.csv_token_logprobs_backward(logits.data_ptr(), ty, ld, N, V, _dense(tokens, "tokens", torch.int32, (N,), dev),
-                                           _dense(stats, "stats", torch.float32, (N, 2), dev), _dense(grad_logp, "grad_logp", torch.float32, (N,), dev),
-                                           inv_temperature, gp, gld, torch._C._cuda_getCurrentRawStream(dev)))
+    _check(lib.csv_token_logprobs_backward(logits.data_ptr(), ty, ld, N, V, _vector(tokens, "tokens", torch.int32, N, dev),
+                                           _vector(stats, "stats", torch.float32, 2 * N, dev), _vector(grad_logp, "grad_logp", torch.float32, N, dev),
+                                           inv_temperature, gp, gld, _raw_stream(dev)))
     return grad
 
 
@@ -602,7 +610,7 @@ def csv_policy_loss(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.
                                    logp, grad, want_grad, scratch)
     ty, dev, ld = _rows(logits, "logits")
     N, V = logits.shape
-    f32, n = torch.float32, (N,)
+    f32 = torch.float32
     if loss is None:
         loss = torch.empty((), dtype=f32, device=dev)
     if logp is None:
@@ -611,11 +619,11 @@ def csv_policy_loss(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.
         grad = torch.empty((N, V), dtype=logits.dtype, device=dev)
     gp, gld = (None, 0) if grad is None else _grad_of(logits, grad, ty, dev)
     keep, ptr, size = _scratch(csv_policy_loss_scratch(N, V), scratch, dev)
-    _check(lib.csv_policy_loss(logits.data_ptr(), ty, ld, N, V, _dense(tokens, "tokens", torch.int32, n, dev), _dense(old_logp, "old_logp", f32, n, dev),
-                               None if ref_logp is None else _dense(ref_logp, "ref_logp", f32, n, dev), _dense(advantages, "advantages", f32, n, dev),
-                               _dense(weights, "weights", f32, n, dev), C.byref(PolicyParams(clip_low, clip_high, beta, inv_temperature)),
-                               _dense(loss, "loss", f32, (), dev), _dense(logp, "logp", f32, n, dev), gp, gld, ptr, size,
-                               torch._C._cuda_getCurrentRawStream(dev)))
+    _check(lib.csv_policy_loss(logits.data_ptr(), ty, ld, N, V, _vector(tokens, "tokens", torch.int32, N, dev), _vector(old_logp, "old_logp", f32, N, dev),
+                               None if ref_logp is None else _vector(ref_logp, "ref_logp", f32, N, dev), _vector(advantages, "advantages", f32, N, dev),
+                               _vector(weights, "weights", f32, N, dev), C.byref(PolicyParams(clip_low, clip_high, beta, inv_temperature)),
+                               _vector(loss, "loss", f32, 1, dev), _vector(logp, "logp", f32, N, dev), gp, gld, ptr, size,
+                               _raw_stream(dev)))
     return loss, logp, grad
 
 

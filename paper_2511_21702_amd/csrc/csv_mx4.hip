@@ -420,8 +420,10 @@ __global__ __launch_bounds__(256, 3) void product_kernel(LogitsArgs a) {
 // pieces of 256 bytes, blocks l / 32 and then 2 + l / 32 of a step.
 // The blocks that share a band ask for its codes at about the same time, so that each of them waits for memory, not for a cache.  Codes are
 // therefore requested four steps ahead, each register again as soon as its products are issued; h comes two steps at a time, one such
-// stage ahead, from global memory to LDS without registers, which are all taken: 128 sums, 64 of codes.  2048 at 128256 x 4096, bf16 logits: 605 us,
-// 3.6 PFLOP/s; the matrix cores are busy half of the cycles at 1.6 GHz, and blocks twice as wide or groups that stay in a cache end there as well.
+// stage ahead, from global memory to LDS without registers, which are all taken: 128 sums, 64 of codes.  2048 at 128256 x 4096, bf16 logits: 610 us,
+// 3.5 PFLOP/s.  Its parts, each taken away in turn: the writes of the logits 95 us, codes that come from memory 50, h from memory 20, all
+// three 130; codes of zeros 85 (the clock, which random codes lower).  Products, LDS reads and barriers alone take 371.  Blocks twice as
+// wide, groups of hidden states that stay in a cache and starts staggered so that writes meet other blocks' products gain nothing.
 template <bool ONCE, typename T>
 __global__ __launch_bounds__(256, 2) void many_kernel(LogitsArgs a) {
     constexpr int OW = 64 + 4;

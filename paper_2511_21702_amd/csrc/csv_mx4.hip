@@ -251,7 +251,8 @@ enum { H_BF16, H_TILES, H_ROUNDED_HERE };
 // hidden states become here (a thread rounds a block: cheaper than a launch, while the block waits for W).
 // Bound by the read of W up to 32 hidden states (64 in 4 bits): 1 at 128256 x 4096 42 us (6.8 TB/s), 32 at 256000 x 4608 with 33 MB of logits 106 us
 // (6.2 TB/s); with more of them in bf16 by the matrix cores: 1024 at 128256 x 4096 830 us (1.3 PFLOP/s, the rate of the largest library products).
-// Past the end of a row or of the batch the last piece or row is read again: codes of W are 0 there, and those hidden states are not stored.
+// Past the end of a row or of the batch the last piece or row is read again: the last stage puts zeros in the row's place, and those hidden
+// states are not stored.
 template <int H, int NT, int RT, int S, bool ONCE, typename T>
 __global__ __launch_bounds__(256, 3) void product_kernel(LogitsArgs a) {
     constexpr bool MX4 = H != H_BF16, HERE = H == H_ROUNDED_HERE;
@@ -307,7 +308,7 @@ __global__ __launch_bounds__(256, 3) void product_kernel(LogitsArgs a) {
             }
         }
     };
-    auto store_h = [&](int buf, int c0) {
+    auto store_h = [&](int buf, int c0, bool end) {
 #pragma unroll
         for (int i = 0; i < HT; ++i) {
             const int p = tid + i * 256;
@@ -328,6 +329,8 @@ __global__ __launch_bounds__(256, 3) void product_kernel(LogitsArgs a) {
                 ((uint8_t*)hscale)[(buf * NT * 64 + p % (NT * 64)) * 4 + c] = (uint8_t)scale;
                 continue;
             }
+            // 0 times an infinity would be a NaN; whole steps behind the row are not multiplied
+            if (!MX4 && end && (c0 + p / (NT * 256)) * CHUNK + (p & 15) * 8 >= a.d) hr[i] = v4u{0, 0, 0, 0};
             lds[buf * HP + (MX4 ? p : p ^ (p >> 4 & 15))] = hr[i];
         }
     };
@@ -379,7 +382,7 @@ __global__ __launch_bounds__(256, 3) void product_kernel(LogitsArgs a) {
 #pragma unroll
     for (int c = 0; c < S; ++c) load_w(c, w[c]);
     for (int st = 0; st < stages - 1; ++st) {
-        store_h(st & 1, st * S);
+        store_h(st & 1, st * S, false);
         take_scales(st * S);
         load_h((st + 1) * S);
         load_scales((st + 1) * S);
@@ -393,7 +396,7 @@ __global__ __launch_bounds__(256, 3) void product_kernel(LogitsArgs a) {
         }
     }
     const int last = stages - 1;                                  // the last stage asks for nothing more
-    store_h(last & 1, last * S);
+    store_h(last & 1, last * S, true);
     take_scales(last * S);
     lds_barrier();
     read_hscales(last & 1);

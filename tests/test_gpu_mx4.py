@@ -220,6 +220,26 @@ def test_values_that_are_not_finite_stay_in_their_row_and_column(act, B):
     head.free()
 
 
+@pytest.mark.parametrize("d", [8, 40, 264, 1032])
+@pytest.mark.parametrize("B", [1, 17, 33, 100])
+def test_an_infinite_end_of_a_hidden_state_is_not_multiplied_with_padding(d, B):
+    """An infinity in the last elements of a row meets those of W alone: the logit is that infinity with W's sign, not a NaN of 0 times it."""
+    csv = _csv()
+    V = 70
+    gen = torch.Generator().manual_seed(d + B)
+    dp = O.padded(d)
+    codes = torch.randint(0, 256, (V, dp // 2), generator=gen, dtype=torch.uint8) | 0x11      # no zeros: the index of a magnitude is odd
+    scales = torch.randint(117, 125, (V, dp // 32), generator=gen, dtype=torch.uint8)
+    W = O.mx4_values(codes.numpy(), scales.numpy(), d)
+    head = csv.csv_mx4_head(codes.cuda(), scales.cuda(), None, d)
+    h = torch.randn(B, d, generator=gen).to(BF16)
+    e = d - 1 - torch.arange(B) % 8
+    h[torch.arange(B), e] = float("inf")
+    got = csv.csv_mx4_logits(head, h.cuda()).cpu().double().numpy()
+    assert (got == np.sign(W[:, e.numpy()]).T * np.inf).all()
+    head.free()
+
+
 def test_scales_at_both_ends_meet_in_the_product():
     csv = _csv()
     V, d, B = 64, 128, 16

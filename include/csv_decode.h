@@ -336,7 +336,7 @@ int csv_mx4_dequantize(const uint8_t* d_codes, const uint8_t* d_scales, int rows
  * A head of 4-bit microscaled rows: V rows of d elements in the format above (csv_mx4_quantize of W, or a checkpoint), laid
  * out once for the matrix cores (what the padding of a row holds does not matter).  d_b DEVICE float32[V] or NULL.  The head keeps copies of its own (about V*d*0.53 bytes): the
  * caller may free codes, scales and bias afterwards.  csv_mx4_head_create synchronises the stream before returning; on
- * error *out is NULL.  d <= CSV_MX4_MAX_D.
+ * error *out is NULL.  d <= CSV_MX4_MAX_D, and V (rounded up to 256) times the padded d below 2^37.
  */
 #define CSV_MX4_MAX_D (1 << 20)
 typedef struct csv_mx4_head csv_mx4_head;
@@ -368,7 +368,9 @@ int csv_mx4_logits(const csv_mx4_head* head, const uint16_t* d_h, int B, int act
  * csv_token_logprobs_backward: d_grad[i, j] = c g_i ([j = t] - exp(c (x_j - m)) / s) for g = d_grad_logp, in the type of the
  * logits, from the d_stats of the forward call; d_grad may be d_logits (then ld_grad = ld).  A row with g_i = 0 is zeros and
  * is not read.  Scratch: csv_token_logprobs_scratch bytes, 16-byte aligned, for the forward call (often none).
+ * N <= CSV_LOSS_MAX_ROWS, here and for the policy loss (more rows: several calls).
  */
+#define CSV_LOSS_MAX_ROWS 4194303
 int csv_token_logprobs_scratch(int N, int V, size_t* bytes);
 int csv_token_logprobs(const void* d_logits, int type, int64_t ld, int N, int V, const int32_t* d_tokens, float inv_temperature,
                        float* d_logp, float* d_stats, void* d_scratch, size_t scratch_bytes, void* stream);

@@ -23,6 +23,7 @@ MAX_K, MAX_CLUSTERS, MAX_BATCH = 1024, 8192, 256
 F32, BF16 = 0, 1
 ACT_BF16, ACT_MX4 = 0, 1
 MX4_MAX_BATCH = 65536
+LOSS_MAX_ROWS = 4194303
 
 EXPORTS = [
     "csv_build_index", "csv_index_from_arrays", "csv_index_export", "csv_index_dims", "csv_index_free",

@@ -395,6 +395,7 @@ __global__ __launch_bounds__(1024) void sum_kernel(const double* __restrict__ te
 // ------------------------------------------------------------------------------------------------ entry points
 static int check_logits(const void* x, int type, int64_t ld, int N, int V, const int32_t* tokens, float c) {
     if (N < 0 || V < 1) { csv_set_error("need N >= 0 and V >= 1 (N=%d, V=%d)", N, V); return CSV_ESHAPE; }
+    if (N > CSV_LOSS_MAX_ROWS) { csv_set_error("N=%d is above %d rows", N, CSV_LOSS_MAX_ROWS); return CSV_ESHAPE; }
     if (type != CSV_F32 && type != CSV_BF16) { csv_set_error("bad element type %d", type); return CSV_EINVAL; }
     if (ld < V) { csv_set_error("row stride %lld is below V=%d", (long long)ld, V); return CSV_ESHAPE; }
     if (!(c > 0.f) || !isfinite(c * LOG2E)) { csv_set_error("inverse temperature %g is not positive and finite", (double)c); return CSV_EINVAL; }
@@ -425,7 +426,7 @@ static int check_scratch(size_t need, const void* p, size_t have) {
 #define GRAD_BLOCKS 16384           // gradients from given statistics have nothing to join: short blocks (us for 509 x 151669 bf16, 2048 x
                                     // 128256 float32: 64, 412 with 4096 blocks, 54, 391 with 16384)
 static inline int parts_of(int N, int V, int most) {
-    const int by_rows = most / (N > 0 ? N : 1), by_length = (V + PART_MIN - 1) / PART_MIN;
+    const int by_rows = most / (N > 0 ? N : 1), by_length = (V - 1) / PART_MIN + 1;
     const int p = by_rows < by_length ? by_rows : by_length;
     return p < 1 ? 1 : p > MAX_PARTS ? MAX_PARTS : p;
 }
@@ -491,10 +492,8 @@ extern "C" int csv_token_logprobs_backward(const void* d_logits, int type, int64
     a.x = d_logits; a.ld = ld; a.N = N; a.V = V; a.tokens = d_tokens; a.c = inv_temperature; a.stats_in = d_stats; a.grad_logp = d_grad_logp;
     a.grad = d_grad; a.ld_grad = ld_grad;
     a.parts = parts_of(N, V, GRAD_BLOCKS);
-    const int64_t n = (int64_t)N * a.parts;
-    if (n > 0x7fffffff) { csv_set_error("N=%d rows are too many blocks", N); return CSV_ESHAPE; }
-    if (type == CSV_F32) grad_kernel<float><<<(unsigned)n, 256, 0, (hipStream_t)stream>>>(a);
-    else grad_kernel<uint16_t><<<(unsigned)n, 256, 0, (hipStream_t)stream>>>(a);
+    if (type == CSV_F32) grad_kernel<float><<<N * a.parts, 256, 0, (hipStream_t)stream>>>(a);
+    else grad_kernel<uint16_t><<<N * a.parts, 256, 0, (hipStream_t)stream>>>(a);
     CSV_LAUNCH_CHECK("grad_kernel");
     return CSV_OK;
 }

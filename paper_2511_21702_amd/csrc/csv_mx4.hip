@@ -566,7 +566,7 @@ static unsigned plan(LogitsArgs& a, int rows, int states) {
     a.blocks = (a.V + rows - 1) / rows;
     a.groups = (a.B + states - 1) / states;
     const int64_t n = (int64_t)(a.blocks + 7) / 8 * 8 * a.groups;
-    if (n <= 0x7fffffff) return (unsigned)n;
+    if (n <= 0xffffff) return (unsigned)n;                       // a launch holds fewer than 2^32 threads
     csv_set_error("V=%d rows x B=%d hidden states are too many blocks", a.V, a.B);
     return 0;
 }
@@ -636,12 +636,13 @@ extern "C" int csv_mx4_head_create(const uint8_t* d_codes, const uint8_t* d_scal
     if (V < 1 || d < 8 || (d & 7) != 0) { csv_set_error("need V >= 1 and d a positive multiple of 8 (V=%d, d=%d)", V, d); return CSV_ESHAPE; }
     if (V > 0x7fffffff - HEAD_ROWS || d > CSV_MX4_MAX_D) { csv_set_error("V=%d or d=%d is too large", V, d); return CSV_ESHAPE; }
     if ((uintptr_t)d_codes & 15) { csv_set_error("codes have to be 16-byte aligned"); return CSV_EINVAL; }
+    const int64_t bands = ((int64_t)V + HEAD_ROWS - 1) / HEAD_ROWS * (HEAD_ROWS / 64), pieces = bands * chunks_of(d) * 256;
+    if (pieces > 0xffffff00LL) { csv_set_error("head of %d x %d: 2^37 padded elements or more", V, d); return CSV_ESHAPE; }
     csv_mx4_head* x = (csv_mx4_head*)calloc(1, sizeof(csv_mx4_head));
     if (!x) { csv_set_error("host allocation failed"); return CSV_ENOMEM; }
     x->V = V;
     x->d = d;
     x->chunks = chunks_of(d);
-    const int64_t bands = ((int64_t)V + HEAD_ROWS - 1) / HEAD_ROWS * (HEAD_ROWS / 64), pieces = bands * x->chunks * 256;
     const hipStream_t st = (hipStream_t)stream;
     hipError_t e = hipGetDevice(&x->device);
     if (e == hipSuccess) e = hipMalloc((void**)&x->bands, (size_t)(bands * band_bytes(x->chunks)));

@@ -81,6 +81,32 @@ def test_logprobs_and_their_gradient(N, V, dtype, gap, shift, c):
     assert torch.equal(x, got)
 
 
+def test_as_many_rows_as_a_call_takes():
+    csv = _csv()
+    N, V = csv.LOSS_MAX_ROWS, 3
+    log(f"logprobs and policy loss N={N} V={V}")
+    x, t = _rows(N, V, F32, 8)
+    logp, stats = csv.csv_token_logprobs(x, t)
+    x64, t64 = x.cpu().double().numpy(), t.cpu().numpy()
+    m, s, want, p = O.rows_logp(x64, t64, 1.0)
+    tol, rel = O.logp_tolerance(x64, m, p, 1.0, want)
+    assert (np.abs(logp.cpu().double().numpy() - want) <= tol).all()
+    g = torch.randn(N, generator=torch.Generator().manual_seed(1))
+    got = csv.csv_token_logprobs_backward(x, t, stats, g.cuda())
+    _grad_close(got.cpu().double().numpy(), p, s, t64, g.double().numpy(), 1.0, rel, x64, m, F32)
+    # at a ratio of exactly 1 the loss is minus the sum of w A, and the gradient that of g = -w A
+    w = torch.full((N,), 2.0 ** -22)
+    loss, lp, grad = csv.csv_policy_loss(x, t, logp, None, g.cuda(), w.cuda())
+    assert torch.equal(lp, logp)
+    # the ratio is off by what rounding the old log-probability to float32 leaves
+    wa = (w.double() * g.double()).numpy()
+    off = np.abs(wa) * np.abs(want) * O.U24 * 1.01
+    assert abs(float(loss) + wa.sum()) <= off.sum() + (abs(wa.sum()) + np.abs(wa).sum()) * O.U24
+    _grad_close(grad.cpu().double().numpy(), p, s, t64, -wa, 1.0, rel, x64, m, F32, relg=np.abs(want) * O.U24 * 1.01)
+    with pytest.raises(csv.CsvError):
+        csv.csv_token_logprobs(torch.zeros(N + 1, 1, device="cuda"), torch.zeros(N + 1, dtype=torch.int32, device="cuda"))
+
+
 def _policy_inputs(logp, N, seed, skip=True):
     rng = np.random.default_rng(seed)
     # ratios away from the clip's borders by more than what a log-probability may be off

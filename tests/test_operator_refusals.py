@@ -112,6 +112,21 @@ def test_loss_refused(csv):
         assert pol(**bad) == EINVAL, bad
 
 
+def test_more_work_than_one_launch_holds_is_refused(csv):
+    out, n = C.c_void_p(77), C.c_size_t()
+    for V, d in ((2 ** 30, 256), (2 ** 31 - 300, 8), (131073, 2 ** 20)):
+        out.value = 77
+        assert csv.lib.csv_mx4_head_create(P, P, None, V, d, None, C.byref(out)) == ESHAPE and out.value is None
+    N, huge = 4194304, 1 << 40
+    assert csv.lib.csv_token_logprobs(P, 0, 4, N, 4, P, 1.0, P, P, P, huge, None) == ESHAPE
+    assert b"4194303" in csv.lib.csv_last_error()
+    assert csv.lib.csv_token_logprobs_backward(P, 0, 4, N, 4, P, P, P, 1.0, P, 4, None) == ESHAPE
+    params = csv.PolicyParams(0.2, 0.2, 0.0, 1.0)
+    assert csv.lib.csv_policy_loss(P, 0, 4, N, 4, P, P, None, P, P, C.byref(params), P, P, None, 0, P, huge, None) == ESHAPE
+    # the longest row there is
+    assert csv.lib.csv_policy_loss_scratch(1, 2 ** 31 - 1, C.byref(n)) == 0 and n.value == 8 + 8 * 64 + 8 + 8
+
+
 def test_binding_refuses_host_tensors_and_wrong_types(csv):
     x = torch.zeros(4, 64)
     with pytest.raises(ValueError):

@@ -169,7 +169,7 @@ struct LogitsArgs {
     const uint8_t* hc;          // or 4-bit tiles of it
     const uint32_t* hs;
     void* out;
-    int wide;                   // rows of the output are 16-byte aligned
+    int lines;                  // rows of the output start at multiples of 64 bytes and are as long
 };
 
 __device__ __forceinline__ v8i widen(const v4u& u) { return v8i{(int)u.x, (int)u.y, (int)u.z, (int)u.w, 0, 0, 0, 0}; }
@@ -189,45 +189,47 @@ __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// The logits of G hidden states from b0 on and RT * 16 rows from row0 on, from a wave's part of LDS, where a hidden state is a row: so
-// that a row of logits is written in one piece per wave.  Logits leave past the caches, which keep W and h (us, without / with: 32 hidden states
-// at 256000 x 4608, float32, 131 / 117; 2048 at 128257 x 1024, 655 / 568).
-template <int G, int RT, typename T>
+// The bias of a block's ROWS rows, one per thread, on its way to LDS.
+template <int ROWS>
+__device__ __forceinline__ float own_bias(const LogitsArgs& a, int64_t row0) {
+    const int64_t row = row0 + threadIdx.x;
+    return threadIdx.x < ROWS && a.bias && row < a.V ? a.bias[row] : 0.f;
+}
+// The logits of G hidden states from b0 on and a block's ROWS rows from row0 on, from LDS, where a hidden state is a row of ROWS + 4 floats.
+// A wave writes whole rows of the block.  Memory takes lines of 64 bytes, and a part of one costs as much as many whole ones, so the 16-byte pieces
+// that leave past the caches (which keep W and h) make up whole lines; what lies before the first line and after the last goes one by one
+// through the cache, where the neighbour's part may still meet it.  2048 hidden states at 128257 x 128, float32, 4 bits / bf16: each wave its own
+// 64 rows, in single logits, 436 / 427 us, so 221 / 317, and 208 where all rows start lines (V = 128256); 128257 x 4096 in 4 bits, bf16 logits, 662 -> 644.
+// Products that are bound by the bf16 matrix rate lose up to 4 percent by it where V is odd, 1 percent at d = 4096.
+template <int G, int ROWS, typename T>
 __device__ __forceinline__ void give_out(const LogitsArgs& a, const float* buf, int64_t b0, int64_t row0) {
-    constexpr int OW = RT * 16 + 4;
-    const int lane = threadIdx.x & 63;
-    __builtin_amdgcn_wave_barrier();
-    constexpr int W = sizeof(T) == 4 ? 4 : 8;                 // logits in 16 bytes
-    if (a.wide) {
-        constexpr int L = RT * 16 / W;                        // lanes of a hidden state
-        const int64_t row = row0 + lane % L * W;
-        if (row < a.V) {
-            float bias[W];
+    constexpr int OW = ROWS + 4, E = 16 / sizeof(T), LINE = 4 * E, L = ROWS / E, P = 64 / L;      // lanes of a row, rows of a wave's pass
+    static_assert(64 % L == 0 && G % (4 * P) == 0, "a wave takes whole rows");
+    const int lane = threadIdx.x & 63, l = lane % L, n = (int)min((int64_t)ROWS, a.V - row0);
+    for (int t = (threadIdx.x >> 6) * P + lane / L; t < G && b0 + t < a.B; t += 4 * P) {
+        T* to = (T*)a.out + (b0 + t) * a.V + row0;
+        const float* from = buf + t * OW;
+        auto piece = [&](int e) {
+            float v[E];
 #pragma unroll
-            for (int i = 0; i < W; ++i) bias[i] = a.bias ? a.bias[row + i] : 0.f;
-            for (int t = lane / L; t < G && b0 + t < a.B; t += 64 / L) {
-                float v[W];
-#pragma unroll
-                for (int i = 0; i < W; ++i) v[i] = buf[t * OW + lane % L * W + i] + bias[i];
-                T* to = (T*)a.out + (b0 + t) * a.V + row;
-                if constexpr (sizeof(T) == 4) __builtin_nontemporal_store(v4f{v[0], v[1], v[2], v[3]}, (v4f*)to);
-                else __builtin_nontemporal_store(v4u{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])}, (v4u*)to);
-            }
+            for (int i = 0; i < E; ++i) v[i] = from[e + i];
+            if constexpr (E == 4) __builtin_nontemporal_store(v4f{v[0], v[1], v[2], v[3]}, (v4f*)(to + e));
+            else __builtin_nontemporal_store(v4u{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])}, (v4u*)(to + e));
+        };
+        if (a.lines) {
+            if (l * E < n) piece(l * E);
+            continue;
         }
-    } else {
-        constexpr int L = RT * 16;
-        const int64_t row = row0 + lane % L;
-        if (row < a.V) {
-            const float bias = a.bias ? a.bias[row] : 0.f;
-            for (int t = lane / L; t < G && b0 + t < a.B; t += 64 / L) {
-                const float v = buf[t * OW + lane % L] + bias;
-                T* to = (T*)a.out + (b0 + t) * a.V + row;
-                if constexpr (sizeof(T) == 4) __builtin_nontemporal_store(v, to);
-                else *to = __builtin_bit_cast(uint16_t, (__bf16)v);
-            }
+        const int head = min(n, (int)(-(uintptr_t)to & 63) / (int)sizeof(T)), pieces = (n - head) / LINE * 4, singles = n - pieces * E;
+        if (l < pieces) piece(head + l * E);
+#pragma unroll
+        for (int k = 0; k < (2 * LINE - 2 + L - 1) / L; ++k) {
+            const int q = l + k * L, e = q < head ? q : q + pieces * E;
+            if (q >= singles) continue;
+            if constexpr (E == 4) to[e] = from[e];
+            else to[e] = __builtin_bit_cast(uint16_t, (__bf16)from[e]);
         }
     }
-    __builtin_amdgcn_wave_barrier();                              // the next group overwrites what this one reads
 }
 
 // Codes that one block alone reads (ONCE: all hidden states in one group) go past the caches: 1 hidden state at 128256 x 4096 53.0 -> 46.4 us, 32 at
@@ -258,9 +260,11 @@ __global__ __launch_bounds__(256, 3) void product_kernel(LogitsArgs a) {
     constexpr bool MX4 = H != H_BF16, HERE = H == H_ROUNDED_HERE;
     constexpr int HP = NT * S * (MX4 ? 64 : 256);                 // 16-byte pieces of a stage of h
     constexpr int HT = (HP + 255) / 256;                          // of them per thread
-    constexpr int OW = RT * 16 + 4;                               // floats per hidden state in a wave's part of the output buffer
-    constexpr int LDS = 2 * HP > 16 * OW ? 2 * HP : 16 * OW;      // four waves' parts
+    constexpr int ROWS = 64 * RT, OW = ROWS + 4;                  // floats per hidden state in the output buffer
+    constexpr int GT = NT > 1 ? 2 : 1;                            // groups of hidden states that leave together
+    constexpr int LDS = 2 * HP > GT * 4 * OW ? 2 * HP : GT * 4 * OW;
     __shared__ v4u lds[LDS];
+    __shared__ v4f bias[ROWS / 4];
     __shared__ uint32_t hscale[HERE ? 2 * NT * 64 : 1];           // of h that is rounded here, a byte per step of the stage
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, col = lane & 15;
     // blocks of one die (every eighth) take the groups of hidden states of one block of rows after each other: W comes from that die's cache
@@ -405,15 +409,22 @@ __global__ __launch_bounds__(256, 3) void product_kernel(LogitsArgs a) {
         if (last * S + c < chunks) products(last & 1, c, w[c]);
 
     // lane l holds rows 4 (l / 16) .. + 3 of hidden state l % 16 of every tile
+    if (tid < ROWS) ((float*)bias)[tid] = own_bias<ROWS>(a, tile0 * 16 - wave * (RT * 16));
     __syncthreads();
-    float* buf = (float*)lds + wave * 16 * OW;
+    float* buf = (float*)lds;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
+    for (int n = 0; n < NT; n += GT) {
         const int64_t b0 = (htile0 + n) * 16;
-        if (b0 >= a.B) continue;
+        if (b0 >= a.B) break;                                     // of the whole block
+        if (n > 0) __syncthreads();
 #pragma unroll
-        for (int r = 0; r < RT; ++r) *(v4f*)(buf + col * OW + r * 16 + g * 4) = acc[r][n];
-        give_out<16, RT, T>(a, buf, b0, tile0 * 16);
+        for (int r = 0; r < RT; ++r) {
+            const int e = (wave * RT + r) * 16 + g * 4;
+#pragma unroll
+            for (int k = 0; k < GT; ++k) *(v4f*)(buf + (k * 16 + col) * OW + e) = acc[r][n + k] + bias[e >> 2];
+        }
+        __syncthreads();
+        give_out<16 * GT, ROWS, T>(a, buf, b0, tile0 * 16 - wave * (RT * 16));
     }
 }
 
@@ -429,11 +440,14 @@ __global__ __launch_bounds__(256, 3) void product_kernel(LogitsArgs a) {
 // wide, groups of hidden states that stay in a cache and starts staggered so that writes meet other blocks' products gain nothing.
 template <bool ONCE, typename T>
 __global__ __launch_bounds__(256, 2) void many_kernel(LogitsArgs a) {
-    constexpr int OW = 64 + 4;
-    __shared__ v4u lds[4 * 32 * OW / 4 > 2 * 1024 + 256 ? 4 * 32 * OW / 4 : 2 * 1024 + 256];
+    constexpr int OW = 256 + 4;
+    static_assert(32 * OW / 4 <= 2 * 1024 + 256, "logits take the place of h");
+    __shared__ v4u lds[2 * 1024 + 256 + 64];                      // one array: with two the compiler waits for h on its way to LDS at every read
+    v4f* bias = (v4f*)(lds + 2 * 1024 + 256);
     uint32_t* hscale = (uint32_t*)(lds + 2 * 1024);               // two buffers of 8 tiles
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int j = blockIdx.x >> 3, group = j % a.groups, block = (j / a.groups) * 8 + (blockIdx.x & 7);
+    // as in product_kernel, but the blocks of rows of a die are neighbours: they share lines of logits
+    const int j = blockIdx.x >> 3, group = j % a.groups, block = (blockIdx.x & 7) * ((a.blocks + 7) >> 3) + j / a.groups;
     if (block >= a.blocks) return;
     const int chunks = a.chunks, quads = (chunks + 3) >> 2;
     const int at = (lane >> 4 & 1) * 64 + (lane >> 5) * 16 + (lane & 15);      // this lane's block in a run of tiles, in lanes
@@ -546,18 +560,23 @@ __global__ __launch_bounds__(256, 2) void many_kernel(LogitsArgs a) {
 
     // lane l holds rows 8 i + 4 (l / 32) .. + 3 of hidden state l % 32 of a block of 32 x 32; h of a stage that was not needed may still be on its way
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    ((float*)bias)[tid] = own_bias<256>(a, (int64_t)block * 256);
     __syncthreads();
-    float* buf = (float*)lds + wave * 32 * OW;
+    float* buf = (float*)lds;
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
         const int64_t b0 = htile0 * 16 + n * 32;
-        if (b0 >= a.B) continue;
+        if (b0 >= a.B) break;                                     // of the whole block
+        if (n > 0) __syncthreads();
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *(v4f*)(buf + (lane & 31) * OW + r * 32 + i * 8 + (lane >> 5) * 4) = v4f{acc[r][n][4 * i], acc[r][n][4 * i + 1], acc[r][n][4 * i + 2], acc[r][n][4 * i + 3]};
-        give_out<32, 4, T>(a, buf, b0, ((int64_t)block * 4 + wave) * 64);
+            for (int i = 0; i < 4; ++i) {
+                const int e = wave * 64 + r * 32 + i * 8 + (lane >> 5) * 4;
+                *(v4f*)(buf + (lane & 31) * OW + e) = v4f{acc[r][n][4 * i], acc[r][n][4 * i + 1], acc[r][n][4 * i + 2], acc[r][n][4 * i + 3]} + bias[e >> 2];
+            }
+        __syncthreads();
+        give_out<32, 256, T>(a, buf, b0, (int64_t)block * 256);
     }
 }
 
@@ -716,7 +735,7 @@ extern "C" int csv_mx4_logits(const csv_mx4_head* x, const uint16_t* d_h, int B,
     const hipStream_t st = (hipStream_t)stream;
     LogitsArgs a = {};
     a.bands = x->bands; a.bias = x->bias; a.V = x->V; a.d = x->d; a.chunks = x->chunks; a.B = B; a.h = d_h; a.out = d_logits;
-    a.wide = ((uintptr_t)d_logits & 15) == 0 && x->V % (out_type == CSV_F32 ? 4 : 8) == 0;
+    a.lines = ((uintptr_t)d_logits & 63) == 0 && x->V % (out_type == CSV_F32 ? 16 : 32) == 0;
     const int64_t tt = tiles_of(B);
     if (need) {
         uint8_t* hc = (uint8_t*)d_scratch;

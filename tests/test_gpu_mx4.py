@@ -220,6 +220,27 @@ def test_values_that_are_not_finite_stay_in_their_row_and_column(act, B):
     head.free()
 
 
+@pytest.mark.parametrize("V,B,act", [(16, 3, 0), (70, 20, 0), (515, 3, 1), (515, 40, 1), (515, 70, 0), (1024, 33, 0), (1999, 4100, 1), (2016, 4100, 1),
+                                     (50001, 5, 0), (100015, 17, 1), (100003, 20, 0)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_logits_may_start_anywhere(V, B, act, dtype):
+    """The place of the logits changes which stores write them, and nothing else: the same values, nothing around them touched."""
+    csv = _csv()
+    log(f"logits at shifts V={V} B={B} act={act} {dtype}")
+    d = 40
+    head, W, b = _head(V, d, V + B)
+    h = torch.randn(B, d, generator=torch.Generator().manual_seed(B)).to(BF16).cuda()
+    want = csv.csv_mx4_logits(head, h, act=act)
+    _check(head, W, b, h.cpu(), act, F32, want)
+    want = want.to(dtype)
+    for shift in (0, 1, 2, 5, 8, 15, 16, 31):
+        mem = torch.full((shift + B * V + 64,), 7.0, dtype=dtype, device="cuda")
+        csv.csv_mx4_logits(head, h, out=mem[shift:shift + B * V].view(B, V), act=act)
+        assert torch.equal(mem[shift:shift + B * V].view(B, V), want), shift
+        assert bool((mem[:shift] == 7.0).all()) and bool((mem[shift + B * V:] == 7.0).all())
+    head.free()
+
+
 @pytest.mark.parametrize("d", [8, 40, 264, 1032])
 @pytest.mark.parametrize("B", [1, 17, 33, 100])
 def test_an_infinite_end_of_a_hidden_state_is_not_multiplied_with_padding(d, B):

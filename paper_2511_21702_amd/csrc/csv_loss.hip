@@ -12,17 +12,18 @@
 // A row starts wherever its stride puts it: it is read as up to E - 1 single elements, 16-byte pieces of E elements, and up to
 // E - 1 single elements (E = 4 or 8); the single ones go to the first threads, one each.
 //
-// Exponentials.  With c2 = c log2(e), exp(c (x - m)) = 2^(x c2 - m c2): one fused multiply-add and one exponential per logit, which matters,
-// because at bfloat16's bytes per logit the instructions cost as much as the memory.  k = m c2 is rounded, by at most 2^-5 while it is
-// below NEAR; what is lost, d = fma(m, c2, -k), is known exactly and taken out of the sum, so that s is relative to m itself.  Rows whose
-// largest logit lies further out (and rows of minus infinities, NaNs and plus infinities) take a second pass that subtracts first.
+// Exponentials.  exp(c (x - m)) = 2^(d c2) with d = x - m and c2 = c log2(e).  c2 as one float32 is off by up to 2^-25 of itself, and with it every
+// log-probability of every row, the same way, by that part of c (m - E[x]).  It is kept as the sum of two floats: fma(d, hi, d lo) rounds once (mean error of
+// 2048 rows of 64007 float32 logits, c = 1 / 0.7: -5.8e-8 / -9.5e-8 with one float, below 1e-8 with two; 64 rows of 128256, bound by instructions, 9.8 ->
+// 11.5 us, many rows, bound by memory, within 1 percent).  The low part cannot be added to a rounded d hi, or to m c2 before it: most of it is
+// lost in their last digit.  A thread adds up in float32;
+// threads and parts are added in float64, because what those last sums lose is not averaged over anything.
 #include "csv_common.h"
 
 #include <math.h>
 
-#define LOG2E 1.44269504089f
+#define LOG2E 1.4426950408889634
 #define LOWEST (-3.402823466e38f)
-#define NEAR 524288.f               // 2^19
 #define MAX_PARTS 64                // parts of a row: one per lane of the wave that joins them
 #define PART_MIN 2048               // logits of a part, at least
 
@@ -32,6 +33,7 @@ struct RowArgs {
     int N, V, parts;
     const int32_t* tokens;
     float c;                 // inverse temperature
+    float2 c2;               // c log2(e), see split()
     const float* old_logp;   // policy loss
     const float* ref_logp;
     const float* adv;
@@ -102,39 +104,77 @@ template <typename T> struct Row {
     }
 };
 
+// A double as two floats, x below it and y > 0: minus infinity times either one is minus infinity, and so is their sum.
+static float2 split(double c2) {
+    float hi = (float)c2;
+    if ((double)hi >= c2) hi = nextafterf(hi, 0.f);
+    const float lo = (float)(c2 - (double)hi);
+    return make_float2(hi, lo > 0.f ? lo : 1.4013e-45f);
+}
 // 2^((x - m) c2)
-__device__ __forceinline__ float exp_far(float x, float m, float c2) { return __builtin_amdgcn_exp2f((x - m) * c2); }
+__device__ __forceinline__ float exp_of(float x, float m, float2 c2) {
+    const float d = x - m;
+    return __builtin_amdgcn_exp2f(fmaf(d, c2.x, d * c2.y));
+}
 
 struct Stat {
-    float m, s;
+    float m;
+    double s;
 };
 
-// m and s of the single elements and the pieces lo .. hi - 1 of a row, by the whole block.  A thread keeps its own maximum and its sum
-// relative to max(m c2, -NEAR): what is masked, by minus infinity or by a number far down, adds 0 wherever it stands.
-// red: >= 16 words of LDS
+// Sums of doubles: a wave's by lane exchanges without LDS, the waves' in one order for all threads.
+template <int CTRL, int ROW_MASK, bool ZERO>
+__device__ __forceinline__ double dpp_add(double v) {
+    const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
+    const int lo = (int)(unsigned)u, hi = (int)(unsigned)(u >> 32);
+    const unsigned a = (unsigned)dpp_move<CTRL, ROW_MASK>(ZERO ? 0 : lo, lo), b = (unsigned)dpp_move<CTRL, ROW_MASK>(ZERO ? 0 : hi, hi);
+    return v + __builtin_bit_cast(double, (unsigned long long)b << 32 | a);
+}
+__device__ __forceinline__ double wave_sum(double v) {
+    v = dpp_add<0xB1, 0xf, false>(v);      // quad_perm [1,0,3,2]
+    v = dpp_add<0x4E, 0xf, false>(v);      // quad_perm [2,3,0,1]
+    v = dpp_add<0x141, 0xf, false>(v);     // row_half_mirror
+    v = dpp_add<0x140, 0xf, false>(v);     // row_mirror
+    v = dpp_add<0x142, 0xa, true>(v);      // row_bcast15 into rows 1 and 3
+    v = dpp_add<0x143, 0xc, true>(v);      // row_bcast31 into rows 2 and 3
+    const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
+    const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)u, 63), hi = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(u >> 32), 63);
+    return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
+}
+template <int THREADS>
+__device__ __forceinline__ double block_sum(double v, double* red) {
+    v = wave_sum(v);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.0;
+    for (int w = 0; w < THREADS / 64; ++w) v += red[w];
+    return v;
+}
+
+// m and s of the single elements and the pieces lo .. hi - 1 of a row, by the whole block.  A thread keeps its own maximum and its sum relative to it.
+// The maximum starts at the lowest number, not at minus infinity, which less itself would be NaN: logits of minus infinity add 0 to any of them.
+// red: >= 16 doubles of LDS
 template <int THREADS, typename T>
-__device__ __forceinline__ Stat fold(const Row<T>& row, int lo, int hi, bool singles, float c2, float* red) {
+__device__ __forceinline__ Stat fold(const Row<T>& row, int lo, int hi, bool singles, float2 c2, double* red) {
     constexpr int E = Vec<T>::E, U = 4;
     const int one = singles ? row.single(threadIdx.x) : -1;
-    float m = -INFINITY, k = -NEAR, s = 0.f;
+    float m = LOWEST, s = 0.f;
     if (one >= 0) {
         const float x = get(row.p + one);
         m = fmaxf(m, x);
-        k = fmaxf(m * c2, -NEAR);
-        s = __builtin_amdgcn_exp2f(fmaf(x, c2, -k));
+        s = exp_of(x, m, c2);
     }
     const T* base = row.p + row.head;
     auto take = [&](const auto& x, int n) {
         float top = m;
         for (int u = 0; u < n; ++u)
             for (int j = 0; j < E; ++j) top = fmaxf(top, x[u].v[j]);
-        const float kn = fmaxf(top * c2, -NEAR);
         float add = 0.f;
         for (int u = 0; u < n; ++u)
-            for (int j = 0; j < E; ++j) add += __builtin_amdgcn_exp2f(fmaf(x[u].v[j], c2, -kn));
-        s = fmaf(s, __builtin_amdgcn_exp2f(k - kn), add);
+            for (int j = 0; j < E; ++j) add += exp_of(x[u].v[j], top, c2);
+        s = fmaf(s, exp_of(m, top, c2), add);
         m = top;
-        k = kn;
     };
     int i = lo + threadIdx.x;
     for (; i + (U - 1) * THREADS < hi; i += U * THREADS) {
@@ -149,30 +189,19 @@ __device__ __forceinline__ Stat fold(const Row<T>& row, int lo, int hi, bool sin
         take(x, 1);
     }
     Stat r;
-    r.m = block_max(m, red);
-    const float mc = r.m * c2, K = fmaxf(mc, -NEAR);
-    r.s = block_sum(s * __builtin_amdgcn_exp2f(k - K), red);
-    if (r.s > 0.f && fabsf(mc) < NEAR) {
-        r.s *= __builtin_amdgcn_exp2f(-fmaf(r.m, c2, -K));
-        return r;
-    }
-    const float base_m = fmaxf(r.m, LOWEST);                    // minus infinity less itself would be NaN
-    s = one >= 0 ? exp_far(get(row.p + one), base_m, c2) : 0.f;
-    for (i = lo + threadIdx.x; i < hi; i += THREADS) {
-        Vec<T> x;
-        x.load(base + (int64_t)i * E);
-        for (int j = 0; j < E; ++j) s += exp_far(x.v[j], base_m, c2);
-    }
-    r.s = block_sum(s, red);
+    r.m = block_max(m, (float*)red);
+    r.s = block_sum<THREADS>((double)(s * exp_of(m, r.m, c2)), red);
+    if (r.s == 0.0) r.m = -INFINITY;       // the largest logit itself adds 1, unless it is minus infinity
     return r;
 }
 
 // c g ([j = t] - p_j) over the single elements and the pieces lo .. hi - 1 of a row; eg = c g
-template <int THREADS, bool FAR, typename T>
-__device__ __forceinline__ void write_part(const Row<T>& row, T* out, int lo, int hi, bool singles, int token, float m, float c2, float eg, float f) {
+template <int THREADS, typename T>
+__device__ __forceinline__ void write_grad(const Row<T>& row, T* out, int lo, int hi, bool singles, int token, float m, double s, float2 c2, float eg) {
     constexpr int E = Vec<T>::E, U = 4;
-    const float k = m * c2;
-    auto value = [&](float x) { return -f * (FAR ? exp_far(x, m, c2) : __builtin_amdgcn_exp2f(fmaf(x, c2, -k))); };
+    const float f = (float)((double)eg / s);
+    // where the result is rounded to bfloat16, 2^-9 of it, what one float32 of c2 loses (2^-23 of the exponent) is not seen
+    auto value = [&](float x) { return -f * (sizeof(T) == 4 ? exp_of(x, m, c2) : __builtin_amdgcn_exp2f((x - m) * c2.x)); };
     const int one = singles ? row.single(threadIdx.x) : -1;
     if (one >= 0) put(out + one, (one == token ? eg : 0.f) + value(get(row.p + one)));
     const T* from = row.p + row.head;
@@ -202,12 +231,6 @@ __device__ __forceinline__ void write_part(const Row<T>& row, T* out, int lo, in
     }
 }
 template <int THREADS, typename T>
-__device__ __forceinline__ void write_grad(const Row<T>& row, T* out, int lo, int hi, bool singles, int token, float m, float s, float c2, float eg) {
-    const float k = m * c2;
-    if (fabsf(k) < NEAR) write_part<THREADS, false>(row, out, lo, hi, singles, token, m, c2, eg, eg / s * __builtin_amdgcn_exp2f(-fmaf(m, c2, -k)));
-    else write_part<THREADS, true>(row, out, lo, hi, singles, token, m, c2, eg, eg / s);
-}
-template <int THREADS, typename T>
 __device__ __forceinline__ void write_zeros(T* out, int V, int part, int parts) {
     const Row<T> row(out, V);
     const int one = part == 0 ? row.single(threadIdx.x) : -1;
@@ -217,7 +240,7 @@ __device__ __forceinline__ void write_zeros(T* out, int V, int part, int parts) 
 }
 
 __device__ __forceinline__ double log_prob(Stat r, float xt, float c) {
-    return r.s == 0.f ? -INFINITY : (double)c * ((double)xt - (double)r.m) - log((double)r.s);
+    return r.s == 0.0 ? -INFINITY : (double)c * ((double)xt - (double)r.m) - log(r.s);
 }
 
 // The loss term of a row and its derivative by the log-probability, in float64: one thread per row does this, and close to a clip border
@@ -245,7 +268,7 @@ __device__ __forceinline__ bool left_out(const RowArgs& a, int i, int token, boo
 // 2048 x 128256: 171 us in float32 (6.1 TB/s), 86 us in bf16.
 template <typename T, bool POLICY>
 __global__ __launch_bounds__(1024, 8) void row_kernel(RowArgs a) {
-    __shared__ float red[16];
+    __shared__ double red[16];
     __shared__ float coef;
     const int i = blockIdx.x, tid = threadIdx.x, token = a.tokens[i];
     T* grad = POLICY && a.grad ? (T*)a.grad + (int64_t)i * a.ld_grad : nullptr;
@@ -259,8 +282,8 @@ __global__ __launch_bounds__(1024, 8) void row_kernel(RowArgs a) {
         return;
     }
     const Row<T> row((const T*)a.x + (int64_t)i * a.ld, a.V);
-    const float c2 = a.c * LOG2E, xt = get(row.p + token);
-    const Stat r = fold<1024>(row, 0, row.pieces, true, c2, red);
+    const float xt = get(row.p + token);
+    const Stat r = fold<1024>(row, 0, row.pieces, true, a.c2, red);
     if (tid == 0) {
         const double logp = log_prob(r, xt, a.c);
         if (a.logp) a.logp[i] = (float)logp;
@@ -270,26 +293,26 @@ __global__ __launch_bounds__(1024, 8) void row_kernel(RowArgs a) {
             coef = (float)(g * (double)a.c);
         } else {
             a.stats[2 * i] = r.m;
-            a.stats[2 * i + 1] = r.s;
+            a.stats[2 * i + 1] = (float)r.s;
         }
     }
     if (!POLICY || !grad) return;
     __syncthreads();                            // the row's token has been read by now: the gradient may replace the logits
-    if (r.s == 0.f) write_zeros<1024>(grad, a.V, 0, 1);
-    else write_grad<1024>(row, grad, 0, row.pieces, true, token, r.m, r.s, c2, coef);
+    if (r.s == 0.0) write_zeros<1024>(grad, a.V, 0, 1);
+    else write_grad<1024>(row, grad, 0, row.pieces, true, token, r.m, r.s, a.c2, coef);
 }
 
 // Short blocks, bound by the latency of a chain of loads and a reduction: 7 x 32003 float32 3.6 us, 64 x 128256 bf16 6.3 us.
 template <typename T, bool POLICY>
 __global__ __launch_bounds__(256, 8) void part_kernel(RowArgs a) {
-    __shared__ float red[16];
+    __shared__ double red[16];
     const int i = blockIdx.x / a.parts, p = blockIdx.x % a.parts, token = a.tokens[i];
     if (POLICY && blockIdx.x == 0 && threadIdx.x == 0) *a.arrived = 0;
     if (left_out(a, i, token, POLICY)) return;
     const Row<T> row((const T*)a.x + (int64_t)i * a.ld, a.V);
-    const Stat r = fold<256>(row, (int)((int64_t)row.pieces * p / a.parts), (int)((int64_t)row.pieces * (p + 1) / a.parts), p == 0, a.c * LOG2E, red);
+    const Stat r = fold<256>(row, (int)((int64_t)row.pieces * p / a.parts), (int)((int64_t)row.pieces * (p + 1) / a.parts), p == 0, a.c2, red);
     if (threadIdx.x == 0) {
-        a.part[(int64_t)i * a.parts + p] = make_float2(r.m, r.s);
+        a.part[(int64_t)i * a.parts + p] = make_float2(r.m, (float)r.s);
         if (p == 0) a.xt[i] = get(row.p + token);
     }
 }
@@ -301,14 +324,14 @@ __device__ __forceinline__ Stat join(const RowArgs& a, int i) {
     if (lane < a.parts) v = a.part[(int64_t)i * a.parts + lane];
     Stat r;
     r.m = wave_max(v.x);
-    r.s = wave_sum(v.y == 0.f ? 0.f : v.y * exp_far(v.x, r.m, a.c * LOG2E));
+    r.s = wave_sum(v.y == 0.f ? 0.0 : (double)v.y * (double)exp_of(v.x, r.m, a.c2));
     return r;
 }
 
 __global__ __launch_bounds__(256) void join_kernel(RowArgs a) {
     const int i = blockIdx.x * 4 + (threadIdx.x >> 6);
     if (i >= a.N) return;
-    Stat r = {0.f, 0.f};
+    Stat r = {0.f, 0.0};
     float logp = 0.f;
     if (!left_out(a, i, a.tokens[i], false)) {
         r = join(a, i);
@@ -317,7 +340,7 @@ __global__ __launch_bounds__(256) void join_kernel(RowArgs a) {
     if ((threadIdx.x & 63) == 0) {
         a.logp[i] = logp;
         a.stats[2 * i] = r.m;
-        a.stats[2 * i + 1] = r.s;
+        a.stats[2 * i + 1] = (float)r.s;
     }
 }
 
@@ -344,7 +367,7 @@ __global__ __launch_bounds__(256) void policy_kernel(RowArgs a, int parts, float
     const int i = blockIdx.x / parts, p = blockIdx.x % parts, token = a.tokens[i];
     T* grad = a.grad ? (T*)a.grad + (int64_t)i * a.ld_grad : nullptr;
     const bool out = left_out(a, i, token, true);
-    Stat r = {0.f, 0.f};
+    Stat r = {0.f, 0.0};
     if (!out) r = join(a, i);
     if (threadIdx.x == 0) {
         double logp = 0.0, g = 0.0, term = 0.0;
@@ -366,8 +389,8 @@ __global__ __launch_bounds__(256) void policy_kernel(RowArgs a, int parts, float
     __syncthreads();
     if (grad) {
         const Row<T> row((const T*)a.x + (int64_t)i * a.ld, a.V);
-        if (out || r.s == 0.f) write_zeros<256>(grad, a.V, p, parts);
-        else write_grad<256>(row, grad, (int)((int64_t)row.pieces * p / parts), (int)((int64_t)row.pieces * (p + 1) / parts), p == 0, token, r.m, r.s, a.c * LOG2E, coef);
+        if (out || r.s == 0.0) write_zeros<256>(grad, a.V, p, parts);
+        else write_grad<256>(row, grad, (int)((int64_t)row.pieces * p / parts), (int)((int64_t)row.pieces * (p + 1) / parts), p == 0, token, r.m, r.s, a.c2, coef);
     }
     if (last) {
         const double s = sum_terms<256>(a.terms, a.N, sums);
@@ -383,7 +406,7 @@ __global__ __launch_bounds__(256) void grad_kernel(RowArgs a) {
     const float m = a.stats_in[2 * i], s = a.stats_in[2 * i + 1], g = a.grad_logp[i] * a.c;
     const Row<T> row((const T*)a.x + (int64_t)i * a.ld, a.V);
     if (left_out(a, i, token, false) || g == 0.f || s == 0.f) write_zeros<256>(grad, a.V, p, a.parts);
-    else write_grad<256>(row, grad, (int)((int64_t)row.pieces * p / a.parts), (int)((int64_t)row.pieces * (p + 1) / a.parts), p == 0, token, m, s, a.c * LOG2E, g);
+    else write_grad<256>(row, grad, (int)((int64_t)row.pieces * p / a.parts), (int)((int64_t)row.pieces * (p + 1) / a.parts), p == 0, token, m, s, a.c2, g);
 }
 
 __global__ __launch_bounds__(1024) void sum_kernel(const double* __restrict__ terms, int N, float* __restrict__ loss) {
@@ -398,7 +421,7 @@ static int check_logits(const void* x, int type, int64_t ld, int N, int V, const
     if (N > CSV_LOSS_MAX_ROWS) { csv_set_error("N=%d is above %d rows", N, CSV_LOSS_MAX_ROWS); return CSV_ESHAPE; }
     if (type != CSV_F32 && type != CSV_BF16) { csv_set_error("bad element type %d", type); return CSV_EINVAL; }
     if (ld < V) { csv_set_error("row stride %lld is below V=%d", (long long)ld, V); return CSV_ESHAPE; }
-    if (!(c > 0.f) || !isfinite(c * LOG2E)) { csv_set_error("inverse temperature %g is not positive and finite", (double)c); return CSV_EINVAL; }
+    if (!(c > 0.f) || !isfinite((float)(c * LOG2E))) { csv_set_error("inverse temperature %g is not positive and finite", (double)c); return CSV_EINVAL; }
     if (N > 0 && (!x || !tokens)) { csv_set_error("null logits or tokens"); return CSV_EINVAL; }
     if (N > 0 && ((uintptr_t)x & (type == CSV_F32 ? 3 : 1))) { csv_set_error("logits are not aligned to their type"); return CSV_EINVAL; }
     return CSV_OK;
@@ -465,7 +488,7 @@ extern "C" int csv_token_logprobs(const void* d_logits, int type, int64_t ld, in
     if (rc || N == 0) return rc;
     if (!d_logp || !d_stats) { csv_set_error("null d_logp or d_stats"); return CSV_EINVAL; }
     RowArgs a = {};
-    a.x = d_logits; a.ld = ld; a.N = N; a.V = V; a.tokens = d_tokens; a.c = inv_temperature; a.logp = d_logp; a.stats = d_stats;
+    a.x = d_logits; a.ld = ld; a.N = N; a.V = V; a.tokens = d_tokens; a.c = inv_temperature; a.c2 = split((double)a.c * LOG2E); a.logp = d_logp; a.stats = d_stats;
     const hipStream_t st = (hipStream_t)stream;
     if (logprobs_by_parts(N, V)) {
         place_scratch(a, d_scratch);
@@ -489,7 +512,7 @@ extern "C" int csv_token_logprobs_backward(const void* d_logits, int type, int64
     if (rc || N == 0) return rc;
     if (!d_stats || !d_grad_logp || !d_grad) { csv_set_error("null d_stats, d_grad_logp or d_grad"); return CSV_EINVAL; }
     RowArgs a = {};
-    a.x = d_logits; a.ld = ld; a.N = N; a.V = V; a.tokens = d_tokens; a.c = inv_temperature; a.stats_in = d_stats; a.grad_logp = d_grad_logp;
+    a.x = d_logits; a.ld = ld; a.N = N; a.V = V; a.tokens = d_tokens; a.c = inv_temperature; a.c2 = split((double)a.c * LOG2E); a.stats_in = d_stats; a.grad_logp = d_grad_logp;
     a.grad = d_grad; a.ld_grad = ld_grad;
     a.parts = parts_of(N, V, GRAD_BLOCKS);
     if (type == CSV_F32) grad_kernel<float><<<N * a.parts, 256, 0, (hipStream_t)stream>>>(a);
@@ -513,7 +536,7 @@ extern "C" int csv_policy_loss(const void* d_logits, int type, int64_t ld, int N
     if (N > 0 && (!d_old_logp || !d_advantages || !d_weights)) { csv_set_error("null d_old_logp, d_advantages or d_weights"); return CSV_EINVAL; }
     if (N > 0 && p->beta > 0.f && !d_ref_logp) { csv_set_error("beta=%g needs d_ref_logp", (double)p->beta); return CSV_EINVAL; }
     RowArgs a = {};
-    a.x = d_logits; a.ld = ld; a.N = N; a.V = V; a.tokens = d_tokens; a.c = p->inv_temperature;
+    a.x = d_logits; a.ld = ld; a.N = N; a.V = V; a.tokens = d_tokens; a.c = p->inv_temperature; a.c2 = split((double)a.c * LOG2E);
     a.old_logp = d_old_logp; a.ref_logp = d_ref_logp; a.adv = d_advantages; a.weights = d_weights;
     a.clip_low = p->clip_low; a.clip_high = p->clip_high; a.beta = p->beta;
     a.logp = d_logp; a.grad = d_grad; a.ld_grad = ld_grad;

@@ -372,10 +372,10 @@ int csv_mx4_logits(const csv_mx4_head* head, const uint16_t* d_h, int B, int act
  */
 #define CSV_LOSS_MAX_ROWS 4194303
 int csv_token_logprobs_scratch(int N, int V, size_t* bytes);
-int csv_token_logprobs(const void* d_logits, int type, int64_t ld, int N, int V, const int32_t* d_tokens, float inv_temperature,
+int csv_token_logprobs(const void* d_logits, int type, int64_t ld, int N, int V, const int32_t* d_tokens, double inv_temperature,
                        float* d_logp, float* d_stats, void* d_scratch, size_t scratch_bytes, void* stream);
 int csv_token_logprobs_backward(const void* d_logits, int type, int64_t ld, int N, int V, const int32_t* d_tokens,
-                                const float* d_stats, const float* d_grad_logp, float inv_temperature, void* d_grad,
+                                const float* d_stats, const float* d_grad_logp, double inv_temperature, void* d_grad,
                                 int64_t ld_grad, void* stream);
 
 /*
@@ -391,10 +391,10 @@ int csv_token_logprobs_backward(const void* d_logits, int type, int64_t ld, int 
  * Scratch: csv_policy_loss_scratch bytes, 16-byte aligned.
  */
 typedef struct {
-    float clip_low;        /* 0..1 */
-    float clip_high;       /* >= 0 (plus infinity: no upper clip) */
-    float beta;            /* >= 0, finite */
-    float inv_temperature; /* > 0, finite */
+    double clip_low;        /* 0..1 */
+    double clip_high;       /* >= 0 (plus infinity: no upper clip) */
+    double beta;            /* >= 0, finite */
+    double inv_temperature; /* > 0, finite (in float32 too) */
 } csv_policy_params;
 int csv_policy_loss_scratch(int N, int V, size_t* bytes);
 int csv_policy_loss(const void* d_logits, int type, int64_t ld, int N, int V, const int32_t* d_tokens,

@@ -56,7 +56,7 @@ class KmaxCtl(C.Structure):
 
 
 class PolicyParams(C.Structure):
-    _fields_ = [("clip_low", C.c_float), ("clip_high", C.c_float), ("beta", C.c_float), ("inv_temperature", C.c_float)]
+    _fields_ = [("clip_low", C.c_double), ("clip_high", C.c_double), ("beta", C.c_double), ("inv_temperature", C.c_double)]
 
 
 class StepOut(C.Structure):
@@ -97,7 +97,7 @@ def _load() -> C.CDLL:
     lib.csv_workspace_set_spin_limit.argtypes = [vp, ci]
     lib.csv_index_use_bf16_centroids.argtypes = [vp, vp]
     lib.csv_workspace_set_tail_split.argtypes = [vp, ci]
-    i64, sz, cf = C.c_int64, C.c_size_t, C.c_float
+    i64, sz, cd = C.c_int64, C.c_size_t, C.c_double
     lib.csv_mx4_quantize.argtypes = [vp, ci, i64, ci, ci, vp, vp, vp]
     lib.csv_mx4_dequantize.argtypes = [vp, vp, ci, ci, vp, ci, i64, vp]
     lib.csv_mx4_head_create.argtypes = [vp, vp, vp, ci, ci, vp, C.POINTER(vp)]
@@ -108,8 +108,8 @@ def _load() -> C.CDLL:
     lib.csv_mx4_logits.argtypes = [vp, vp, ci, ci, vp, ci, vp, sz, vp]
     lib.csv_token_logprobs_scratch.argtypes = [ci, ci, C.POINTER(sz)]
     lib.csv_policy_loss_scratch.argtypes = [ci, ci, C.POINTER(sz)]
-    lib.csv_token_logprobs.argtypes = [vp, ci, i64, ci, ci, vp, cf, vp, vp, vp, sz, vp]
-    lib.csv_token_logprobs_backward.argtypes = [vp, ci, i64, ci, ci, vp, vp, vp, cf, vp, i64, vp]
+    lib.csv_token_logprobs.argtypes = [vp, ci, i64, ci, ci, vp, cd, vp, vp, vp, sz, vp]
+    lib.csv_token_logprobs_backward.argtypes = [vp, ci, i64, ci, ci, vp, vp, vp, cd, vp, i64, vp]
     lib.csv_policy_loss.argtypes = [vp, ci, i64, ci, ci, vp, vp, vp, vp, vp, C.POINTER(PolicyParams), vp, vp, vp, i64, vp, sz, vp]
     return lib
 

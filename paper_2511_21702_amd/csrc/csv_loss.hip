@@ -32,13 +32,13 @@ struct RowArgs {
     int64_t ld;
     int N, V, parts;
     const int32_t* tokens;
-    float c;                 // inverse temperature
+    double c;                // inverse temperature
     float2 c2;               // c log2(e), see split()
     const float* old_logp;   // policy loss
     const float* ref_logp;
     const float* adv;
     const float* weights;
-    float clip_low, clip_high, beta;
+    double clip_low, clip_high, beta;
     const float* stats_in;   // gradient alone
     const float* grad_logp;
     float* logp;
@@ -239,21 +239,21 @@ __device__ __forceinline__ void write_zeros(T* out, int V, int part, int parts) 
     for (int i = (int)((int64_t)row.pieces * part / parts) + threadIdx.x; i < hi; i += THREADS) __builtin_nontemporal_store(v4u{0, 0, 0, 0}, (v4u*)(out + row.head + (int64_t)i * Vec<T>::E));
 }
 
-__device__ __forceinline__ double log_prob(Stat r, float xt, float c) {
-    return r.s == 0.0 ? -INFINITY : (double)c * ((double)xt - (double)r.m) - log(r.s);
+__device__ __forceinline__ double log_prob(Stat r, float xt, double c) {
+    return r.s == 0.0 ? -INFINITY : c * ((double)xt - (double)r.m) - log(r.s);
 }
 
 // The loss term of a row and its derivative by the log-probability, in float64: one thread per row does this, and close to a clip border
 // the digits decide which branch holds.
 __device__ __forceinline__ double policy_term(const RowArgs& a, int i, double logp, double& g) {
     const double A = a.adv[i], w = a.weights[i], r = exp(logp - (double)a.old_logp[i]);
-    const double lo = 1.0 - (double)a.clip_low, hi = 1.0 + (double)a.clip_high, whole = r * A, cut = fmin(fmax(r, lo), hi) * A;
+    const double lo = 1.0 - a.clip_low, hi = 1.0 + a.clip_high, whole = r * A, cut = fmin(fmax(r, lo), hi) * A;
     double term = cut < whole ? -cut : -whole;
     double d = (A >= 0.0 ? r > hi : r < lo) ? 0.0 * A : -whole;      // a NaN of the inputs is one of the gradient too
-    if (a.beta > 0.f) {
+    if (a.beta > 0.0) {
         const double k = (double)a.ref_logp[i] - logp, em = expm1(k);
-        term += (double)a.beta * (em - k);
-        d -= (double)a.beta * em;
+        term += a.beta * (em - k);
+        d -= a.beta * em;
     }
     g = w * d;
     return w * term;
@@ -290,7 +290,7 @@ __global__ __launch_bounds__(1024, 8) void row_kernel(RowArgs a) {
         if (POLICY) {
             double g;
             a.terms[i] = policy_term(a, i, logp, g);
-            coef = (float)(g * (double)a.c);
+            coef = (float)(g * a.c);
         } else {
             a.stats[2 * i] = r.m;
             a.stats[2 * i + 1] = (float)r.s;
@@ -375,7 +375,7 @@ __global__ __launch_bounds__(256) void policy_kernel(RowArgs a, int parts, float
             logp = log_prob(r, a.xt[i], a.c);
             term = policy_term(a, i, logp, g);
         }
-        coef = (float)(g * (double)a.c);
+        coef = (float)(g * a.c);
         last = 0;
         if (p == 0) {
             if (a.logp) a.logp[i] = (float)logp;
@@ -403,7 +403,7 @@ template <typename T>
 __global__ __launch_bounds__(256) void grad_kernel(RowArgs a) {
     const int i = blockIdx.x / a.parts, p = blockIdx.x % a.parts, token = a.tokens[i];
     T* grad = (T*)a.grad + (int64_t)i * a.ld_grad;
-    const float m = a.stats_in[2 * i], s = a.stats_in[2 * i + 1], g = a.grad_logp[i] * a.c;
+    const float m = a.stats_in[2 * i], s = a.stats_in[2 * i + 1], g = (float)((double)a.grad_logp[i] * a.c);
     const Row<T> row((const T*)a.x + (int64_t)i * a.ld, a.V);
     if (left_out(a, i, token, false) || g == 0.f || s == 0.f) write_zeros<256>(grad, a.V, p, a.parts);
     else write_grad<256>(row, grad, (int)((int64_t)row.pieces * p / a.parts), (int)((int64_t)row.pieces * (p + 1) / a.parts), p == 0, token, m, s, a.c2, g);
@@ -416,12 +416,12 @@ __global__ __launch_bounds__(1024) void sum_kernel(const double* __restrict__ te
 }
 
 // ------------------------------------------------------------------------------------------------ entry points
-static int check_logits(const void* x, int type, int64_t ld, int N, int V, const int32_t* tokens, float c) {
+static int check_logits(const void* x, int type, int64_t ld, int N, int V, const int32_t* tokens, double c) {
     if (N < 0 || V < 1) { csv_set_error("need N >= 0 and V >= 1 (N=%d, V=%d)", N, V); return CSV_ESHAPE; }
     if (N > CSV_LOSS_MAX_ROWS) { csv_set_error("N=%d is above %d rows", N, CSV_LOSS_MAX_ROWS); return CSV_ESHAPE; }
     if (type != CSV_F32 && type != CSV_BF16) { csv_set_error("bad element type %d", type); return CSV_EINVAL; }
     if (ld < V) { csv_set_error("row stride %lld is below V=%d", (long long)ld, V); return CSV_ESHAPE; }
-    if (!(c > 0.f) || !isfinite((float)(c * LOG2E))) { csv_set_error("inverse temperature %g is not positive and finite", (double)c); return CSV_EINVAL; }
+    if (!(c > 0.0) || !isfinite((float)(c * LOG2E)) || !(split(c * LOG2E).x > 0.f)) { csv_set_error("inverse temperature %g is not positive and finite in float32", c); return CSV_EINVAL; }
     if (N > 0 && (!x || !tokens)) { csv_set_error("null logits or tokens"); return CSV_EINVAL; }
     if (N > 0 && ((uintptr_t)x & (type == CSV_F32 ? 3 : 1))) { csv_set_error("logits are not aligned to their type"); return CSV_EINVAL; }
     return CSV_OK;
@@ -479,7 +479,7 @@ static void place_scratch(RowArgs& a, void* p) {
     a.arrived = (int*)(a.xt + 2 * (size_t)a.N);
 }
 
-extern "C" int csv_token_logprobs(const void* d_logits, int type, int64_t ld, int N, int V, const int32_t* d_tokens, float inv_temperature, float* d_logp,
+extern "C" int csv_token_logprobs(const void* d_logits, int type, int64_t ld, int N, int V, const int32_t* d_tokens, double inv_temperature, float* d_logp,
                                   float* d_stats, void* d_scratch, size_t have, void* stream) {
     int rc = check_logits(d_logits, type, ld, N, V, d_tokens, inv_temperature);
     size_t need = 0;
@@ -488,7 +488,7 @@ extern "C" int csv_token_logprobs(const void* d_logits, int type, int64_t ld, in
     if (rc || N == 0) return rc;
     if (!d_logp || !d_stats) { csv_set_error("null d_logp or d_stats"); return CSV_EINVAL; }
     RowArgs a = {};
-    a.x = d_logits; a.ld = ld; a.N = N; a.V = V; a.tokens = d_tokens; a.c = inv_temperature; a.c2 = split((double)a.c * LOG2E); a.logp = d_logp; a.stats = d_stats;
+    a.x = d_logits; a.ld = ld; a.N = N; a.V = V; a.tokens = d_tokens; a.c = inv_temperature; a.c2 = split(a.c * LOG2E); a.logp = d_logp; a.stats = d_stats;
     const hipStream_t st = (hipStream_t)stream;
     if (logprobs_by_parts(N, V)) {
         place_scratch(a, d_scratch);
@@ -506,13 +506,13 @@ extern "C" int csv_token_logprobs(const void* d_logits, int type, int64_t ld, in
 }
 
 extern "C" int csv_token_logprobs_backward(const void* d_logits, int type, int64_t ld, int N, int V, const int32_t* d_tokens, const float* d_stats,
-                                           const float* d_grad_logp, float inv_temperature, void* d_grad, int64_t ld_grad, void* stream) {
+                                           const float* d_grad_logp, double inv_temperature, void* d_grad, int64_t ld_grad, void* stream) {
     int rc = check_logits(d_logits, type, ld, N, V, d_tokens, inv_temperature);
     if (!rc) rc = check_grad(d_logits, type, ld, N, V, d_grad, ld_grad);
     if (rc || N == 0) return rc;
     if (!d_stats || !d_grad_logp || !d_grad) { csv_set_error("null d_stats, d_grad_logp or d_grad"); return CSV_EINVAL; }
     RowArgs a = {};
-    a.x = d_logits; a.ld = ld; a.N = N; a.V = V; a.tokens = d_tokens; a.c = inv_temperature; a.c2 = split((double)a.c * LOG2E); a.stats_in = d_stats; a.grad_logp = d_grad_logp;
+    a.x = d_logits; a.ld = ld; a.N = N; a.V = V; a.tokens = d_tokens; a.c = inv_temperature; a.c2 = split(a.c * LOG2E); a.stats_in = d_stats; a.grad_logp = d_grad_logp;
     a.grad = d_grad; a.ld_grad = ld_grad;
     a.parts = parts_of(N, V, GRAD_BLOCKS);
     if (type == CSV_F32) grad_kernel<float><<<N * a.parts, 256, 0, (hipStream_t)stream>>>(a);
@@ -531,12 +531,12 @@ extern "C" int csv_policy_loss(const void* d_logits, int type, int64_t ld, int N
     if (!rc) rc = csv_policy_loss_scratch(N, V, &need);
     if (!rc) rc = check_scratch(need, d_scratch, have);
     if (rc) return rc;
-    if (!(p->clip_low >= 0.f && p->clip_low <= 1.f) || !(p->clip_high >= 0.f)) { csv_set_error("clip range 1 - %g .. 1 + %g", (double)p->clip_low, (double)p->clip_high); return CSV_EINVAL; }
-    if (!(p->beta >= 0.f) || !isfinite(p->beta)) { csv_set_error("beta=%g is negative or not finite", (double)p->beta); return CSV_EINVAL; }
+    if (!(p->clip_low >= 0.0 && p->clip_low <= 1.0) || !(p->clip_high >= 0.0)) { csv_set_error("clip range 1 - %g .. 1 + %g", p->clip_low, p->clip_high); return CSV_EINVAL; }
+    if (!(p->beta >= 0.0) || !isfinite(p->beta)) { csv_set_error("beta=%g is negative or not finite", p->beta); return CSV_EINVAL; }
     if (N > 0 && (!d_old_logp || !d_advantages || !d_weights)) { csv_set_error("null d_old_logp, d_advantages or d_weights"); return CSV_EINVAL; }
-    if (N > 0 && p->beta > 0.f && !d_ref_logp) { csv_set_error("beta=%g needs d_ref_logp", (double)p->beta); return CSV_EINVAL; }
+    if (N > 0 && p->beta > 0.0 && !d_ref_logp) { csv_set_error("beta=%g needs d_ref_logp", p->beta); return CSV_EINVAL; }
     RowArgs a = {};
-    a.x = d_logits; a.ld = ld; a.N = N; a.V = V; a.tokens = d_tokens; a.c = p->inv_temperature; a.c2 = split((double)a.c * LOG2E);
+    a.x = d_logits; a.ld = ld; a.N = N; a.V = V; a.tokens = d_tokens; a.c = p->inv_temperature; a.c2 = split(a.c * LOG2E);
     a.old_logp = d_old_logp; a.ref_logp = d_ref_logp; a.adv = d_advantages; a.weights = d_weights;
     a.clip_low = p->clip_low; a.clip_high = p->clip_high; a.beta = p->beta;
     a.logp = d_logp; a.grad = d_grad; a.ld_grad = ld_grad;

@@ -108,3 +108,39 @@ def test_policy_loss_whose_terms_cancel(N, V, dtype):
     log(f"loss {loss:.3e} exact {exact:.3e}")
     assert abs(exact) < 1e-6
     assert abs(loss - exact) <= COMMON * slope.sum().item() + 6 * ((slope * sigma[:half]) ** 2).sum().sqrt().item() + U * abs(exact) + 1e-15
+
+
+def _with_left_out(rows, values, N):
+    """Vectors of N rows: the given ones first, the rest of weight 0 (the last vector)."""
+    out = []
+    for v, rest in values:
+        t = torch.full((N,), rest, device="cuda")
+        t[:rows] = torch.tensor(v, device="cuda")
+        out.append(t)
+    return out
+
+
+@pytest.mark.parametrize("N", [2, 130])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_parameters_keep_the_digits_of_a_double(N, dtype):
+    """Rows whose log-probabilities are exact, so that temperature, clip and beta are all that a loss can be off by."""
+    csv = _csv()
+    log(f"parameters as doubles N={N} {dtype}")
+    x = torch.zeros(N, 2, dtype=dtype, device="cuda")
+    x[:, 1] = -1000.0                                       # log-probability of token 1: c times that, what is added to it is below 2^-1000
+    t = torch.ones(N, dtype=torch.int32, device="cuda")
+    # temperature: 0.7 times 1000 is 700 to 1e-13, a ratio of 1 to as much; 0.7 as a float32 makes it 1 + 1.2e-5
+    old, adv, w = _with_left_out(2, [([-700.0] * 2, 0.0), ([1.0] * 2, 0.0), ([0.5] * 2, 0.0)], N)
+    loss, logp, _ = csv.csv_policy_loss(x, t, old, None, adv, w, inv_temperature=0.7)
+    assert abs(loss.item() + 1.0) <= 2.0 ** -24 and logp[0].item() == -700.0
+    # clip: 0.5 times 1.2 less 0.75 times 0.8, ratios far beyond either border
+    old, adv, w = _with_left_out(2, [([-1002.0, -998.0], 0.0), ([1.0, -1.0], 0.0), ([0.5, 0.75], 0.0)], N)
+    loss = csv.csv_policy_loss(x, t, old, None, adv, w, clip_low=0.2, clip_high=0.2)[0].item()
+    assert abs(loss) <= 4 * 2.0 ** -53
+    # beta: a term of 0.1 (e - 2) in both rows, and advantages that add up to them as far as two float32 can
+    v = 2 * 0.1 * (math.e - 2.0)
+    a0 = torch.tensor(v, dtype=F32).item()
+    a1 = torch.tensor(v - a0, dtype=F32).item()
+    old, ref, adv, w = _with_left_out(2, [([-1000.0] * 2, 0.0), ([-999.0] * 2, 0.0), ([a0, a1], 0.0), ([1.0] * 2, 0.0)], N)
+    loss = csv.csv_policy_loss(x, t, old, ref, adv, w, beta=0.1)[0].item()
+    assert abs(loss - (v - a0 - a1)) <= 16 * 2.0 ** -53

@@ -313,7 +313,8 @@ int csv_kmax_update(csv_kmax_ctl* c, int n_fallback, int n_sequences);
  * (csv_mx4_head_create and csv_mx4_head_free excepted), so they may be captured into a graph; scratch is the caller's
  * and holds nothing between calls: calls that may overlap (other streams, other graphs) need scratch of their own.
  * Zero rows are a valid request.  A pointer that a call does not need may be NULL.  The current device has to be the
- * one the pointers and the stream belong to.
+ * one the pointers and the stream belong to.  What a call writes (scratch too) shares no memory with what it reads or with
+ * what else it writes, but for a gradient in place of the logits; the calls on log-probabilities and losses refuse it.
  */
 #define CSV_F32  0   /* element types: float32 */
 #define CSV_BF16 1   /*                bfloat16 bit patterns */

@@ -432,6 +432,52 @@ static int check_grad(const void* x, int type, int64_t ld, int N, int V, const v
     if (N > 1 && grad == x && ld_grad != ld) { csv_set_error("a gradient in place of the logits needs their row stride"); return CSV_EINVAL; }
     return CSV_OK;
 }
+
+// Memory of a call: rows of `bytes`, `step` bytes apart.
+struct Span {
+    const char* name;
+    uintptr_t at;
+    int64_t rows, bytes, step;
+    bool in_place;           // logits, and the gradient that may take their place
+};
+static Span vec(const char* name, const void* p, int64_t bytes) { return {name, (uintptr_t)p, bytes > 0, bytes, bytes, false}; }
+static Span matrix(const char* name, const void* p, int type, int64_t ld, int N, int V) {
+    const int64_t e = type == CSV_F32 ? 4 : 2;
+    return {name, (uintptr_t)p, N, V * e, ld * e, true};
+}
+static bool row_meets(uintptr_t at, int64_t bytes, const Span& m) {
+    if (at + bytes <= m.at || at >= m.at + (m.rows - 1) * m.step + m.bytes) return false;
+    const int64_t r = at < m.at ? 0 : (int64_t)((at - m.at) % m.step);      // beyond a row's end there is another row
+    return r < m.bytes || r + bytes > m.step;
+}
+static bool meet(const Span& a, const Span& b) {
+    if (!a.at || !b.at || a.rows < 1 || b.rows < 1) return false;
+    if (a.rows == 1) return row_meets(a.at, a.bytes, b);
+    if (b.rows == 1) return row_meets(b.at, b.bytes, a);
+    const uintptr_t a_end = a.at + (a.rows - 1) * a.step + a.bytes, b_end = b.at + (b.rows - 1) * b.step + b.bytes;
+    if (a.at >= b_end || b.at >= a_end) return false;
+    if (a.step == b.step) {               // row j of b begins r bytes behind the start of row j + q of a
+        const int64_t o = (int64_t)(b.at - a.at), r = ((o % a.step) + a.step) % a.step, q = (o - r) / a.step;
+        return (r < a.bytes && q > -b.rows && q < a.rows) || (r + b.bytes > a.step && q + 1 > -b.rows && q + 1 < a.rows);
+    }
+    for (int64_t j = 0; j < b.rows; ++j)
+        if (row_meets(b.at + j * b.step, b.bytes, a)) return true;
+    return false;
+}
+// What a call writes is apart from what it reads and from what else it writes: blocks read while others write.  A gradient in place of the logits
+// is no such case: an element is read by the thread that writes it, and the row's token and statistics before that.
+template <int W, int R>
+static int check_apart(const Span (&writes)[W], const Span (&reads)[R]) {
+    for (int i = 0; i < W; ++i) {
+        for (int j = 0; j < R; ++j) {
+            if (writes[i].in_place && reads[j].in_place && writes[i].at == reads[j].at) continue;      // with one stride: check_grad
+            if (meet(writes[i], reads[j])) { csv_set_error("%s overlaps %s", writes[i].name, reads[j].name); return CSV_EINVAL; }
+        }
+        for (int j = i + 1; j < W; ++j)
+            if (meet(writes[i], writes[j])) { csv_set_error("%s overlaps %s", writes[i].name, writes[j].name); return CSV_EINVAL; }
+    }
+    return CSV_OK;
+}
 static int check_scratch(size_t need, const void* p, size_t have) {
     if (need && (!p || have < need)) { csv_set_error("scratch of %zu bytes, %zu are needed", p ? have : (size_t)0, need); return CSV_ESHAPE; }
     if (need && ((uintptr_t)p & 15)) { csv_set_error("scratch has to be 16-byte aligned"); return CSV_EINVAL; }
@@ -487,6 +533,9 @@ extern "C" int csv_token_logprobs(const void* d_logits, int type, int64_t ld, in
     if (!rc) rc = check_scratch(need, d_scratch, have);
     if (rc || N == 0) return rc;
     if (!d_logp || !d_stats) { csv_set_error("null d_logp or d_stats"); return CSV_EINVAL; }
+    const Span writes[] = {vec("d_logp", d_logp, 4ll * N), vec("d_stats", d_stats, 8ll * N), vec("d_scratch", need ? d_scratch : nullptr, (int64_t)need)};
+    const Span reads[] = {matrix("d_logits", d_logits, type, ld, N, V), vec("d_tokens", d_tokens, 4ll * N)};
+    if ((rc = check_apart(writes, reads))) return rc;
     RowArgs a = {};
     a.x = d_logits; a.ld = ld; a.N = N; a.V = V; a.tokens = d_tokens; a.c = inv_temperature; a.c2 = split(a.c * LOG2E); a.logp = d_logp; a.stats = d_stats;
     const hipStream_t st = (hipStream_t)stream;
@@ -511,6 +560,10 @@ extern "C" int csv_token_logprobs_backward(const void* d_logits, int type, int64
     if (!rc) rc = check_grad(d_logits, type, ld, N, V, d_grad, ld_grad);
     if (rc || N == 0) return rc;
     if (!d_stats || !d_grad_logp || !d_grad) { csv_set_error("null d_stats, d_grad_logp or d_grad"); return CSV_EINVAL; }
+    const Span writes[] = {matrix("d_grad", d_grad, type, ld_grad, N, V)};
+    const Span reads[] = {matrix("d_logits", d_logits, type, ld, N, V), vec("d_tokens", d_tokens, 4ll * N), vec("d_stats", d_stats, 8ll * N),
+                          vec("d_grad_logp", d_grad_logp, 4ll * N)};
+    if ((rc = check_apart(writes, reads))) return rc;
     RowArgs a = {};
     a.x = d_logits; a.ld = ld; a.N = N; a.V = V; a.tokens = d_tokens; a.c = inv_temperature; a.c2 = split(a.c * LOG2E); a.stats_in = d_stats; a.grad_logp = d_grad_logp;
     a.grad = d_grad; a.ld_grad = ld_grad;
@@ -535,6 +588,11 @@ extern "C" int csv_policy_loss(const void* d_logits, int type, int64_t ld, int N
     if (!(p->beta >= 0.0) || !isfinite(p->beta)) { csv_set_error("beta=%g is negative or not finite", p->beta); return CSV_EINVAL; }
     if (N > 0 && (!d_old_logp || !d_advantages || !d_weights)) { csv_set_error("null d_old_logp, d_advantages or d_weights"); return CSV_EINVAL; }
     if (N > 0 && p->beta > 0.0 && !d_ref_logp) { csv_set_error("beta=%g needs d_ref_logp", p->beta); return CSV_EINVAL; }
+    const int64_t n4 = 4ll * N;
+    const Span writes[] = {vec("d_loss", d_loss, 4), vec("d_logp", d_logp, n4), matrix("d_grad", d_grad, type, ld_grad, N, V), vec("d_scratch", d_scratch, (int64_t)need)};
+    const Span reads[] = {matrix("d_logits", d_logits, type, ld, N, V), vec("d_tokens", d_tokens, n4), vec("d_old_logp", d_old_logp, n4),
+                          vec("d_ref_logp", p->beta > 0.0 ? d_ref_logp : nullptr, n4), vec("d_advantages", d_advantages, n4), vec("d_weights", d_weights, n4)};
+    if ((rc = check_apart(writes, reads))) return rc;
     RowArgs a = {};
     a.x = d_logits; a.ld = ld; a.N = N; a.V = V; a.tokens = d_tokens; a.c = p->inv_temperature; a.c2 = split(a.c * LOG2E);
     a.old_logp = d_old_logp; a.ref_logp = d_ref_logp; a.adv = d_advantages; a.weights = d_weights;

@@ -378,3 +378,35 @@ def test_rollout_head_in_four_bits_then_policy_loss_on_the_exact_head():
     ws.free()
     idx.free()
     head.free()
+
+
+@pytest.mark.parametrize("N,V", [(3, 80003), (130, 5000), (1, 4097)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_outputs_may_lie_between_the_rows_of_the_logits(N, V, dtype):
+    """One buffer of rows: logits, their gradient beside them, and the log-probabilities behind both in the first row's gap."""
+    csv = _csv()
+    log(f"side by side N={N} V={V} {dtype}")
+    x, t = _rows(N, V, dtype, 3)
+    old, adv, w = torch.full((N,), -4.0, device="cuda"), torch.linspace(-1, 1, N, device="cuda"), torch.full((N,), 1.0 / N, device="cuda")
+    gap = 2 * N + 8                                      # bfloat16 elements or more for N float32, wherever they start
+    wide = torch.full((N, 2 * V + gap), 7.0, dtype=dtype, device="cuda")
+    wide[:, :V] = x
+    at = wide[0, 2 * V:]
+    at = at[(-(at.data_ptr() // at.element_size())) % (4 // at.element_size()):]
+    logp = at[:4 * N // at.element_size()].view(F32)
+    assert logp.numel() == N
+    loss, _, grad = csv.csv_policy_loss(wide[:, :V], t, old, None, adv, w, logp=logp, grad=wide[:, V:2 * V])
+    # the same alignment of the rows: the same order of sums
+    same = wide.clone()
+    want = csv.csv_policy_loss(same[:, :V], t, old, None, adv, w, grad=same.new_empty(N, 2 * V + gap)[:, V:2 * V])
+    assert torch.equal(loss, want[0]) and torch.equal(logp, want[1]) and torch.equal(grad, want[2])
+    assert torch.equal(wide[:, :V], x)
+    lp, stats = csv.csv_token_logprobs(wide[:, :V], t)
+    wide[:, V:2 * V] = 7.0
+    got = csv.csv_token_logprobs_backward(wide[:, :V], t, stats, adv, grad=wide[:, V:2 * V])
+    assert torch.equal(got, csv.csv_token_logprobs_backward(same[:, :V], t, stats, adv, grad=same.new_empty(N, 2 * V + gap)[:, V:2 * V]))
+    assert torch.equal(wide[:, :V], x)
+    with pytest.raises(csv.CsvError, match="d_logp overlaps d_old_logp"):
+        csv.csv_policy_loss(x, t, old, None, adv, w, logp=old)
+    with pytest.raises(csv.CsvError, match="d_grad overlaps d_logits"):
+        csv.csv_policy_loss(wide[:, :V], t, old, None, adv, w, grad=wide[:, V - 1:2 * V - 1])

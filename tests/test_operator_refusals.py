@@ -167,3 +167,62 @@ def test_policy_formula_against_differences():
             xm[i, j] -= h
             # second differences of the loss are below 40: h^2 times that, and the cancellation of values near 1
             assert abs((loss(xp) - loss(xm)) / (2 * h) - g[i, j]) < 40 * h * h + 1e-10
+
+
+def test_outputs_that_share_memory_are_refused(csv):
+    """One block of a row reads what another one writes: an output may not lie in an input or in another output, by as little as a byte."""
+    A = 1 << 24                                                    # addresses this far apart do not meet
+    N, V = 5, 1000
+
+    def fwd(**k):
+        a = dict(x=A, t=2 * A, logp=3 * A, stats=4 * A, scr=5 * A)
+        a.update(k)
+        n = C.c_size_t()
+        assert csv.lib.csv_token_logprobs_scratch(N, 80000, C.byref(n)) == 0 and n.value >= N * 8
+        return csv.lib.csv_token_logprobs(a["x"], 0, 80000, N, 80000, a["t"], 1.0, a["logp"], a["stats"], a["scr"], 1 << 20, None)
+
+    def bwd(ty=0, N=N, ld=V, ldg=V, **k):
+        a = dict(x=A, t=2 * A, stats=3 * A, g=4 * A, grad=5 * A)
+        a.update(k)
+        return csv.lib.csv_token_logprobs_backward(a["x"], ty, ld, N, V, a["t"], a["stats"], a["g"], 1.0, a["grad"], ldg, None)
+
+    def pol(ty=0, N=N, ld=V, ldg=V, beta=0.1, **k):
+        a = dict(x=A, t=2 * A, old=3 * A, ref=4 * A, adv=5 * A, w=6 * A, loss=7 * A, logp=8 * A, grad=9 * A, scr=10 * A)
+        a.update(k)
+        p = csv.PolicyParams(0.2, 0.2, beta, 1.0)
+        return csv.lib.csv_policy_loss(a["x"], ty, ld, N, V, a["t"], a["old"], a["ref"], a["adv"], a["w"], C.byref(p), a["loss"], a["logp"], a["grad"], ldg,
+                                       a["scr"], 1 << 20, None)
+
+    def refused(rc, first, second):
+        assert rc == EINVAL
+        assert csv.lib.csv_last_error().decode() == f"{first} overlaps {second}"
+
+    for N_ in (5, 300):                                            # rows in parts, one block per row
+        for name, at in (("d_old_logp", 3 * A), ("d_ref_logp", 4 * A), ("d_advantages", 5 * A), ("d_weights", 6 * A), ("d_tokens", 2 * A)):
+            for off in (0, 4 * (N_ - 1), -4 * (N_ - 1)):
+                refused(pol(N=N_, logp=at + off), "d_logp", name)
+            refused(pol(N=N_, loss=at + 4), "d_loss", name)
+            refused(pol(N=N_, grad=at - 4 * N_ * V + 4), "d_grad", name)
+            refused(pol(N=N_, scr=at - 16), "d_scratch", name)
+        refused(pol(N=N_, logp=A + 4 * V), "d_logp", "d_logits")
+        refused(pol(N=N_, logp=7 * A), "d_loss", "d_logp")
+        refused(pol(N=N_, logp=9 * A + 4), "d_logp", "d_grad")
+        refused(pol(N=N_, loss=10 * A), "d_loss", "d_scratch")
+        for f in (bwd, pol):
+            for off in (4, -4, 4 * V, -4 * V, 4 * N_ * V - 4, 4 - 4 * N_ * V):
+                refused(f(N=N_, grad=A + off), "d_grad", "d_logits")
+            refused(f(N=N_, ty=1, grad=A + 2), "d_grad", "d_logits")
+            # rows with a gap: what lies in the gap is apart, what reaches out of it is not
+            for off in (4 * V - 4, 4, 4 * V + 4, 4 * (2 * V) * (N_ - 1) + 4 * V - 4, -4 * (2 * V) * (N_ - 1) + 4, -4 * (2 * V) * (N_ - 1) - 4 * V + 4):
+                refused(f(N=N_, ld=2 * V, ldg=2 * V, grad=A + off), "d_grad", "d_logits")
+            # other strides: some row meets one
+            refused(f(N=N_, ld=2 * V, ldg=2 * V + 1, grad=A + 4 * V), "d_grad", "d_logits")
+            refused(f(N=N_, ld=3 * V, ldg=V, grad=A + 4 * V), "d_grad", "d_logits")
+    refused(bwd(grad=3 * A), "d_grad", "d_stats")
+    refused(bwd(grad=4 * A), "d_grad", "d_grad_logp")
+    refused(bwd(N=1, grad=A + 4), "d_grad", "d_logits")
+    refused(fwd(logp=2 * A), "d_logp", "d_tokens")
+    refused(fwd(stats=2 * A - 4), "d_stats", "d_tokens")
+    refused(fwd(stats=3 * A + 16), "d_logp", "d_stats")
+    refused(fwd(logp=A + 100), "d_logp", "d_logits")
+    refused(fwd(scr=4 * A), "d_stats", "d_scratch")

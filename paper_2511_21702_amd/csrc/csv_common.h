@@ -122,10 +122,15 @@ struct csv_workspace {
 // ---------------------------------------------------------------------------------------------- errors
 void csv_set_error(const char* fmt, ...);
 
+// The runtime keeps an error until it is asked for it, through later calls that succeed.  One that a call has reported is taken back here, or the
+// next launch check on the same thread would report it again, of a kernel that runs.
+static inline void csv_take_error() { (void)hipGetLastError(); }
+
 #define CSV_HIP(call)                                                                       \
     do {                                                                                    \
         hipError_t e_ = (call);                                                             \
         if (e_ != hipSuccess) {                                                             \
+            csv_take_error();                                                               \
             csv_set_error("%s failed: %s (%s:%d)", #call, hipGetErrorString(e_), __FILE__, __LINE__); \
             return CSV_EHIP;                                                                \
         }                                                                                   \

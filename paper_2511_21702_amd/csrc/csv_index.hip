@@ -1355,6 +1355,7 @@ int csv_index_alloc(int V, int d, int C, csv_index** out) {
     A((void**)&x->n, (size_t)C * 4); A((void**)&x->off, (size_t)(C + 1) * 4); A((void**)&x->lnn, (size_t)C * 4);
     A((void**)&x->cmeta, (size_t)C * sizeof(int4));
     if (e != hipSuccess) {
+        csv_take_error();
         csv_set_error("index allocation failed: %s", hipGetErrorString(e));
         csv_index_free(x);
         return e == hipErrorOutOfMemory ? CSV_ENOMEM : CSV_EHIP;
@@ -1398,9 +1399,9 @@ __global__ __launch_bounds__(256) void centroid_bf16_kernel(float* __restrict__ 
 
 static int store_centroids_bf16(csv_index* x, int check, hipStream_t st) {
     const size_t n = (size_t)x->C * x->d;
-    if (!x->mu16 && hipMalloc((void**)&x->mu16, n * 2) != hipSuccess) { csv_set_error("out of device memory (bf16 centroids)"); return CSV_ENOMEM; }
+    if (!x->mu16 && hipMalloc((void**)&x->mu16, n * 2) != hipSuccess) { csv_take_error(); csv_set_error("out of device memory (bf16 centroids)"); return CSV_ENOMEM; }
     int* d_bad = nullptr;
-    if (hipMalloc((void**)&d_bad, 4) != hipSuccess) { csv_set_error("out of device memory"); return CSV_ENOMEM; }
+    if (hipMalloc((void**)&d_bad, 4) != hipSuccess) { csv_take_error(); csv_set_error("out of device memory"); return CSV_ENOMEM; }
     int h_bad = 0;
     hipError_t e = hipMemsetAsync(d_bad, 0, 4, st);
     if (e == hipSuccess) {
@@ -1410,7 +1411,7 @@ static int store_centroids_bf16(csv_index* x, int check, hipStream_t st) {
     if (e == hipSuccess) e = hipMemcpyAsync(&h_bad, d_bad, 4, hipMemcpyDeviceToHost, st);
     if (e == hipSuccess) e = hipStreamSynchronize(st);
     (void)hipFree(d_bad);
-    if (e != hipSuccess) { csv_set_error("bf16 centroid conversion failed: %s", hipGetErrorString(e)); return CSV_EHIP; }
+    if (e != hipSuccess) { csv_take_error(); csv_set_error("bf16 centroid conversion failed: %s", hipGetErrorString(e)); return CSV_EHIP; }
     if (h_bad) {
         (void)hipFree(x->mu16);
         x->mu16 = nullptr;
@@ -1627,6 +1628,7 @@ extern "C" int csv_build_index(const uint16_t* d_W, const float* d_b, int V, int
                  o_d2row = take(bt_m ? (size_t)V * 8 : 0), o_nrm = take(sph ? (size_t)V * 8 : near_rows * 8), o_sums = take(sph ? (size_t)C * d * 8 : 0),
                  o_ext = take(sph ? (size_t)3 * C * 8 : 0);
     auto fail = [&](int code) {
+        csv_take_error();
         if (arena) {
             (void)hipStreamSynchronize(st);
             (void)hipFree(arena);
@@ -1726,9 +1728,9 @@ extern "C" int csv_build_index(const uint16_t* d_W, const float* d_b, int V, int
     }
     std::vector<int32_t> n(C);
     if (launched) launched = hipMemcpyAsync(n.data(), x->n, (size_t)C * 4, hipMemcpyDeviceToHost, st) == hipSuccess;
-    const bool synced = hipStreamSynchronize(st) == hipSuccess;
+    const hipError_t synced = hipStreamSynchronize(st);
     if (!launched) { csv_set_error("launch of the radius kernels failed"); return fail(CSV_EHIP); }
-    if (!synced) { csv_set_error("index build failed on the device: %s", hipGetErrorString(hipGetLastError())); return fail(CSV_EHIP); }
+    if (synced != hipSuccess) { csv_set_error("index build failed on the device: %s", hipGetErrorString(synced)); return fail(CSV_EHIP); }
     {
         int nmax = 1;
         for (int c = 0; c < C; ++c) nmax = n[c] > nmax ? n[c] : nmax;
@@ -1764,7 +1766,7 @@ extern "C" int csv_index_from_arrays(const uint16_t* d_W, const float* d_b, int 
     csv_index* x = nullptr;
     rc = csv_index_alloc(V, d, C, &x);
     if (rc) return rc;
-    auto fail = [&](int code) { csv_index_free(x); return code; };
+    auto fail = [&](int code) { csv_take_error(); csv_index_free(x); return code; };
     {
         int nmax = 1;
         for (int c = 0; c < C; ++c) nmax = n[c] > nmax ? n[c] : nmax;
@@ -1806,7 +1808,7 @@ extern "C" int csv_index_set_bias_table(csv_index* x, int m, const float* h_tabl
     }
     if (m == 0) return CSV_OK;
     const size_t bytes = (size_t)x->C * m * sizeof(float2);
-    if (hipMalloc((void**)&x->bt, bytes) != hipSuccess) { csv_set_error("out of device memory (bias table)"); return CSV_ENOMEM; }
+    if (hipMalloc((void**)&x->bt, bytes) != hipSuccess) { csv_take_error(); csv_set_error("out of device memory (bias table)"); return CSV_ENOMEM; }
     CSV_HIP(hipMemcpyAsync(x->bt, h_table, bytes, hipMemcpyHostToDevice, st));
     CSV_HIP(hipStreamSynchronize(st));
     x->bt_m = m;
@@ -1832,7 +1834,7 @@ extern "C" int csv_index_set_angular(csv_index* x, const float* h_ang, void* str
         return CSV_OK;
     }
     if (x->bt || x->mu16) { csv_set_error("an angular index takes neither a bias table nor bf16 centroids"); return CSV_EINVAL; }
-    if (!x->ang && hipMalloc((void**)&x->ang, (size_t)x->C * sizeof(float4)) != hipSuccess) { csv_set_error("out of device memory (angular metadata)"); return CSV_ENOMEM; }
+    if (!x->ang && hipMalloc((void**)&x->ang, (size_t)x->C * sizeof(float4)) != hipSuccess) { csv_take_error(); csv_set_error("out of device memory (angular metadata)"); return CSV_ENOMEM; }
     CSV_HIP(hipMemcpyAsync(x->ang, h_ang, (size_t)x->C * sizeof(float4), hipMemcpyHostToDevice, st));
     CSV_HIP(hipStreamSynchronize(st));
     return CSV_OK;

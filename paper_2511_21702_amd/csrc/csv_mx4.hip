@@ -673,6 +673,7 @@ extern "C" int csv_mx4_head_create(const uint8_t* d_codes, const uint8_t* d_scal
     }
     if (e == hipSuccess) e = hipStreamSynchronize(st);
     if (e != hipSuccess) {
+        csv_take_error();
         csv_set_error("head of %d x %d: %s", V, d, hipGetErrorString(e));
         csv_mx4_head_free(x);
         return e == hipErrorOutOfMemory ? CSV_ENOMEM : CSV_EHIP;

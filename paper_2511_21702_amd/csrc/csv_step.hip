@@ -3738,6 +3738,7 @@ extern "C" int csv_workspace_create(const csv_index* idx, int B_max, int K_cap_r
         ws->fused_ok = few_per_cu >= 1 && many_per_cu >= 1;
     }
     if (e != hipSuccess) {
+        csv_take_error();
         csv_set_error("workspace allocation failed: %s", hipGetErrorString(e));
         csv_workspace_free(ws);
         return e == hipErrorOutOfMemory ? CSV_ENOMEM : CSV_EHIP;
@@ -3786,6 +3787,7 @@ static int static_scratch(int dev, void** out) {
         const hipError_t e = hipGetSymbolAddress(&p, HIP_SYMBOL(scratch));
         if (e != hipSuccess || !p) {
             pthread_mutex_unlock(&g_scratch_lock);
+            csv_take_error();
             csv_set_error("hipGetSymbolAddress(scratch) failed on device %d: %s", dev, hipGetErrorString(e));
             return CSV_EHIP;
         }
@@ -4033,6 +4035,7 @@ extern "C" int csv_profile_begin(csv_workspace* ws, int max_steps) {
     for (size_t i = 0; i < n; ++i) {
         hipError_t e = hipEventCreate(&ws->prof_ev[i]);
         if (e != hipSuccess) {
+            csv_take_error();
             csv_set_error("hipEventCreate failed: %s", hipGetErrorString(e));
             profile_release(ws);
             return CSV_EHIP;
@@ -4056,6 +4059,7 @@ extern "C" int csv_profile_end(csv_workspace* ws, float* h_stage_ms, int* h_step
             h_stage_ms[i] += ms;
         }
         if (e != hipSuccess) {
+            csv_take_error();
             csv_set_error("event timing failed: %s", hipGetErrorString(e));
             rc = CSV_EHIP;
         }

@@ -387,7 +387,11 @@ int csv_token_logprobs_backward(const void* d_logits, int type, int64_t ld, int 
  *   d_grad[i, j] = g_i c ([j = t_i] - p_ij),   g_i = w_i ( -A_i r_i [A_i >= 0 ? r_i <= 1 + clip_high : r_i >= 1 - clip_low] + beta (1 - exp(k_i)) ).
  * d_logp (or NULL) returns logp.  d_grad (or NULL: the loss alone) has the type of the logits and may be d_logits (then ld_grad =
  * ld).  A row of weight 0, or of a token outside 0..V-1, is left out: nothing of it is read, d_logp 0, a gradient row of zeros.
- * A row of minus infinities has logp minus infinity and a gradient row of zeros.  d_ref_logp is not read where beta is 0.
+ * A row of minus infinities has logp minus infinity, adds nothing to the loss and has a gradient row of zeros.  A token that is itself masked (its
+ * logit minus infinity, others not) has logp minus infinity, r = 0 whatever d_old_logp is, and a gradient row of zeros: no other logit changes it;
+ * its KL term is 0 where d_ref_logp is minus infinity as well, else plus infinity, and so is the loss.  An advantage of 0 adds 0 however large r is.
+ * d_old_logp of minus infinity for a token that is not masked is a ratio of plus infinity: clipped with an advantage above 0, a loss of plus
+ * infinity and a gradient row that is not finite below.  d_ref_logp is not read where beta is 0.
  * The sum over rows is in float64 and in one order: equal calls (with rows at equal alignments) give equal bits.
  * Scratch: csv_policy_loss_scratch bytes, 16-byte aligned.
  */

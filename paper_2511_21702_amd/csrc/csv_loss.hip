@@ -244,18 +244,20 @@ __device__ __forceinline__ double log_prob(Stat r, float xt, double c) {
 }
 
 // The loss term of a row and its derivative by the log-probability, in float64: one thread per row does this, and close to a clip border
-// the digits decide which branch holds.
+// the digits decide which branch holds.  A log-probability of minus infinity is that of a masked token, which no other logit changes: ratio 0, no
+// derivative.  What would be a difference of equal infinities or 0 times a ratio beyond the largest number is taken for 0.
 __device__ __forceinline__ double policy_term(const RowArgs& a, int i, double logp, double& g) {
-    const double A = a.adv[i], w = a.weights[i], r = exp(logp - (double)a.old_logp[i]);
-    const double lo = 1.0 - a.clip_low, hi = 1.0 + a.clip_high, whole = r * A, cut = fmin(fmax(r, lo), hi) * A;
+    const bool masked = isinf(logp);
+    const double A = a.adv[i], w = a.weights[i], old = a.old_logp[i], r = masked && isinf(old) ? 0.0 : exp(logp - old);
+    const double lo = 1.0 - a.clip_low, hi = 1.0 + a.clip_high, whole = A == 0.0 && isinf(r) ? 0.0 : r * A, cut = fmin(fmax(r, lo), hi) * A;
     double term = cut < whole ? -cut : -whole;
     double d = (A >= 0.0 ? r > hi : r < lo) ? 0.0 * A : -whole;      // a NaN of the inputs is one of the gradient too
     if (a.beta > 0.0) {
-        const double k = (double)a.ref_logp[i] - logp, em = expm1(k);
-        term += a.beta * (em - k);
+        const double ref = a.ref_logp[i], k = ref == logp ? 0.0 : ref - logp, em = expm1(k);
+        term += a.beta * (isinf(em) ? em : em - k);
         d -= a.beta * em;
     }
-    g = w * d;
+    g = masked ? 0.0 : w * d;
     return w * term;
 }
 
@@ -288,8 +290,8 @@ __global__ __launch_bounds__(1024, 8) void row_kernel(RowArgs a) {
         const double logp = log_prob(r, xt, a.c);
         if (a.logp) a.logp[i] = (float)logp;
         if (POLICY) {
-            double g;
-            a.terms[i] = policy_term(a, i, logp, g);
+            double g = 0.0;
+            a.terms[i] = r.s == 0.0 ? 0.0 : policy_term(a, i, logp, g);
             coef = (float)(g * a.c);
         } else {
             a.stats[2 * i] = r.m;
@@ -373,7 +375,7 @@ __global__ __launch_bounds__(256) void policy_kernel(RowArgs a, int parts, float
         double logp = 0.0, g = 0.0, term = 0.0;
         if (!out) {
             logp = log_prob(r, a.xt[i], a.c);
-            term = policy_term(a, i, logp, g);
+            if (r.s != 0.0) term = policy_term(a, i, logp, g);
         }
         coef = (float)(g * a.c);
         last = 0;

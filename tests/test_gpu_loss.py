@@ -410,3 +410,58 @@ def test_outputs_may_lie_between_the_rows_of_the_logits(N, V, dtype):
         csv.csv_policy_loss(x, t, old, None, adv, w, logp=old)
     with pytest.raises(csv.CsvError, match="d_grad overlaps d_logits"):
         csv.csv_policy_loss(wide[:, :V], t, old, None, adv, w, grad=wide[:, V - 1:2 * V - 1])
+
+
+@pytest.mark.parametrize("N,V", [(12, 1003), (12, 80003), (200, 1003)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("beta", [0.0, 0.1])
+def test_policy_loss_of_masked_rows_and_masked_tokens(N, V, dtype, beta):
+    """Rows that a mask leaves nothing of, tokens that are masked themselves, and what they were scored with: minus infinity too."""
+    csv = _csv()
+    log(f"masked rows and tokens N={N} V={V} {dtype} beta={beta}")
+    x, t = _rows(N, V, dtype, 9)
+    t[:] = torch.where(t < V // 2, t, t - V // 2)
+    x[:, V // 2 + 1:] = -float("inf")                    # masked in every row
+    x[1] = -float("inf")                                 # nothing left
+    x[2] = -float("inf")
+    t[3:6] = V - 1                                       # the token is masked
+    old, _ = csv.csv_token_logprobs(x, t)
+    assert bool(torch.isneginf(old[1:6]).all()) and bool(torch.isfinite(old[6:]).all())
+    ref = old + 0.25
+    old[2], old[4], ref[2] = -3.0, -3.0, -3.0            # scored as if they were not
+    adv = torch.linspace(-1.0, 1.5, N, device="cuda")
+    adv[3], adv[4], adv[5], adv[6], adv[7] = 0.5, -2.0, -1.0, 0.0, 1.0
+    old[6] = -900.0                                      # a ratio beyond the largest double, advantage 0
+    old[7] = -float("inf")                               # and plus infinity, clipped
+    w = torch.full((N,), 1.0 / N, device="cuda")
+    loss, logp, grad = csv.csv_policy_loss(x, t, old, ref, adv, w, clip_low=0.25, clip_high=0.5, beta=beta)
+    assert bool(torch.isneginf(logp[1:6]).all())
+    assert bool((grad[1:6] == 0).all()) and bool(torch.isfinite(grad.float()).all()) and bool((grad[:, V // 2 + 1:] == 0).all())
+    # the same from the definition: rows 1 and 2 add nothing, 3 to 5 a ratio of 0 (advantage below 0: the clip's border), row 6 its KL term alone
+    x64, t64, A = x.cpu().double().numpy(), t.cpu().numpy(), adv.cpu().double().numpy()
+    m, s, lp, p = O.rows_logp(x64, t64, 1.0)
+    rest = [0] + list(range(8, N))
+    o64, r64 = old.cpu().double().numpy(), ref.cpu().double().numpy()
+    terms = np.zeros(N)
+    terms[rest] = O.policy(lp[rest], o64[rest], r64[rest], A[rest], 1.0, 0.25, 0.5, beta)[0]
+    terms[4], terms[5], terms[7] = 0.75 * 2.0, 0.75 * 1.0, -1.5
+    for i in (6, 7):
+        k = r64[i] - lp[i]
+        terms[i] += beta * (np.exp(k) - k - 1)
+    slope = np.abs(A) * 1.01 + beta * 0.3                # ratios are 1, k is 0.25
+    rel = np.zeros(N)
+    rel[rest + [6, 7]] = O.logp_tolerance(x64[rest + [6, 7]], m[rest + [6, 7]], p[rest + [6, 7]], 1.0, lp[rest + [6, 7]])[1]
+    w1 = float(w[0])
+    # old and ref are rounded to float32 and known; w is what the kernel reads
+    assert abs(float(loss) - w1 * terms.sum()) <= w1 * (slope * rel).sum() * 1.01 + abs(w1 * terms.sum()) * O.U24 + 1e-12
+    assert bool((grad[6] == 0).all()) if beta == 0 else bool(grad[6].any())
+    alone = csv.csv_policy_loss(x, t, old, ref, adv, w, clip_low=0.25, clip_high=0.5, beta=beta, want_grad=False)[0]
+    assert torch.equal(alone, loss)
+    if beta > 0:                                         # the reference knows a token that the policy has masked
+        ref[3] = -3.0
+        loss, logp, grad = csv.csv_policy_loss(x, t, old, ref, adv, w, clip_low=0.25, clip_high=0.5, beta=beta)
+        assert float(loss) == float("inf") and bool((grad[3] == 0).all()) and bool(torch.isfinite(grad.float()).all())
+    # a token that was masked when it was scored, is not now, and is not wanted
+    adv[7] = -1.0
+    loss, logp, grad = csv.csv_policy_loss(x, t, old, old if beta == 0 else ref, adv, w, clip_low=0.25, clip_high=0.5, beta=beta)
+    assert float(loss) == float("inf") and bool(torch.isfinite(grad[8:].float()).all()) and not bool(torch.isfinite(grad[7].float()).all())

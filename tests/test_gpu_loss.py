@@ -465,3 +465,35 @@ def test_policy_loss_of_masked_rows_and_masked_tokens(N, V, dtype, beta):
     adv[7] = -1.0
     loss, logp, grad = csv.csv_policy_loss(x, t, old, old if beta == 0 else ref, adv, w, clip_low=0.25, clip_high=0.5, beta=beta)
     assert float(loss) == float("inf") and bool(torch.isfinite(grad[8:].float()).all()) and not bool(torch.isfinite(grad[7].float()).all())
+
+
+@pytest.mark.parametrize("N,V", [(17000, 130003), (100, 22000003)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_zeros_of_left_out_rows_beyond_32_bits(N, V, dtype):
+    """More than 2^31 logits, all of them NaN in rows that are left out: each of their gradient's elements is written."""
+    csv = _csv()
+    log(f"zeros beyond 32 bits N={N} V={V} {dtype}")
+    x = torch.full((N, V), float("nan"), dtype=dtype, device="cuda")
+    t = torch.full((N,), 7, dtype=torch.int32, device="cuda")
+    w, z = torch.zeros(N, device="cuda"), torch.zeros(N, device="cuda")
+    x[N // 2] = 0.0                                      # one row counts: its gradient is that of a uniform distribution
+    w[N // 2] = 1.0
+    loss, logp, grad = csv.csv_policy_loss(x, t, z - float(np.log(V)), None, z + 1.0, w, grad=x)
+    assert abs(float(loss) + 1.0) < 1e-4
+    rows = [i for i in range(0, N, 1000 if N > 1000 else 1)]
+    assert all(not bool(grad[i:min(i + 1000, N // 2)].any()) for i in rows if i < N // 2)
+    assert all(not bool(grad[max(i, N // 2 + 1):i + 1000].any()) for i in rows)
+    assert bool((grad[N // 2] != 0).all())
+    # the gradient of log-probabilities alone: rows with a gradient of 0 are zeros
+    x.fill_(float("nan"))
+    stats = torch.ones(N, 2, device="cuda")
+    stats[:, 0] = 0.0
+    stats[:, 1] = float(V)
+    x[N - 1] = 0.0
+    g = z.clone()
+    g[N - 1] = 1.0
+    grad = csv.csv_token_logprobs_backward(x, t, stats, g, grad=x)
+    assert all(not bool(grad[i:min(i + 1000, N - 1)].any()) for i in rows)
+    assert bool((grad[N - 1] != 0).all())
+    del x, grad
+    torch.cuda.empty_cache()

@@ -371,3 +371,31 @@ def test_captured_steps_and_a_stream_of_their_own(act, B):
         for k in range(2):
             assert torch.equal(outs[k], eager[(i + k) % 3])
     head.free()
+
+
+@pytest.mark.parametrize("act", [0, 1])
+@pytest.mark.parametrize("B", [3, 40, 80])
+@pytest.mark.parametrize("V", [200, 50003])
+def test_products_below_the_normal_range_are_added_up(act, B, V):
+    """Rows at the smallest scale, 2^-127: every product is subnormal or close to it, and the sums are right to float32's smallest step, 2^-149."""
+    csv = _csv()
+    d = 264
+    log(f"subnormal products V={V} act={act} B={B}")
+    gen = torch.Generator().manual_seed(V + B)
+    dp = O.padded(d)
+    codes = torch.randint(0, 256, (V, dp // 2), generator=gen, dtype=torch.uint8)
+    scales = torch.zeros((V, dp // 32), dtype=torch.uint8)
+    W = O.mx4_values(codes.numpy(), scales.numpy(), d)
+    head = csv.csv_mx4_head(codes.cuda(), scales.cuda(), None, d)
+    h = torch.randn(B, d, generator=gen).to(BF16)
+    h[1] *= 2.0 ** -6                                    # products that are subnormal to the last one
+    got = csv.csv_mx4_logits(head, h.cuda(), act=act).cpu().double().numpy()
+    h64 = O.bf16_values(h)
+    if act:
+        h64 = O.mx4_values(*O.mx4_quantize(h64), d)
+    want = h64 @ W.T
+    # as everywhere, dp roundings of float32 sums; a rounding below the normal range is half a step of 2^-149
+    tol = (dp + 1) * (O.U24 * (np.abs(h64) @ np.abs(W).T) + 2.0 ** -150)
+    assert (np.abs(want) > 20 * tol).mean() > 0.99       # a sum that was lost would show
+    assert (np.abs(got - want) <= tol).all(), np.abs(got - want).max()
+    head.free()

@@ -486,13 +486,18 @@ static int check_scratch(size_t need, const void* p, size_t have) {
     return CSV_OK;
 }
 
-// Where the rows alone leave compute units without work, or with too little of it to keep the memory busy, a row is cut into parts.  Below
-// FEW_ROWS two launches over parts win, though they read the logits twice, from FEW_ROWS on one block per row does (policy loss, us,
-// parts / row: 64 rows of 128256 bf16 14.5 / 20.7, 100 of them 19.0 / 21.4, 128 23.0 / 21.9, 190 30.2 / 25.7).  Without a gradient one block per
-// row is one launch, and stays ahead up to longer rows the more rows there are (parts / row: 1 row of 32000 float32 6.1 / 4.3, of 128256
-// 6.6 / 8.1, 32 of 128256 8.5 / 9.6, 64 of 128256 11.2 / 9.9, 64 of 256000 bf16 12.0 / 14.5).
+// Where the rows alone leave compute units without work, or with too little of it to keep the memory busy, a row is cut into parts: two launches,
+// and the logits are read twice.  A policy loss does so below few_rows (with gradient, us on the GPU, parts / row: rows of 128256 bf16, 64 of them
+// 14.8 / 22.7, 112 20.9 / 24.6, 128 23.2 / 26.7, 190 30.8 / 29.2, of 80000 128 16.6 / 17.4, 160 20.6 / 17.9;  of 128256 float32 64 20.7 / 27.2,
+// 112 32.8 / 33.4, 128 40.4 / 34.8;  of 32000 64 10.5 / 11.8 and 11.0 / 10.8, 112 12.3 / 12.0 and 12.8 / 10.9.  The loss alone follows, so that it
+// keeps its bits: of 128256 bf16 64 10.7 / 12.7, 128 14.5 / 13.9, float32 64 12.2 / 14.4, 90 15.5 / 14.8, of 32000 64 8.7 / 8.1).  Log-probabilities in
+// one block per row are one launch, 3.3 us less for a host that waits for each call, and stay ahead up to longer rows the more rows there are
+// (1 row of 32000 float32 4.8 / 4.6, of 80000 5.0 / 7.2, of 128256 5.0 / 9.6, 64 of 80000 8.0 / 7.7, of 128256 9.7 / 11.7, 90 of 128256
+// 12.4 / 12.2, of 256000 19.4 / 19.2).
 #define FEW_ROWS 112
-#define LONG_ROW(N) (65000 + 1500 * (N))
+#define FEW_ROWS_BF16 144           // the larger one, and what scratch is made for
+static inline int few_rows(int type) { return type == CSV_BF16 ? FEW_ROWS_BF16 : FEW_ROWS; }
+#define LONG_ROW(N) (65000 + 950 * (N))
 #define PART_BLOCKS 2048            // blocks of 256 threads that are resident together
 #define GRAD_BLOCKS 16384           // gradients from given statistics have nothing to join: short blocks (us for 509 x 151669 bf16, 2048 x
                                     // 128256 float32: 64, 412 with 4096 blocks, 54, 391 with 16384)
@@ -510,7 +515,7 @@ static int scratch_bytes(int N, int V, bool parts, size_t* bytes) {
 }
 static inline bool logprobs_by_parts(int N, int V) { return N < FEW_ROWS && V > LONG_ROW(N); }
 
-extern "C" int csv_policy_loss_scratch(int N, int V, size_t* bytes) { return scratch_bytes(N, V, N < FEW_ROWS, bytes); }
+extern "C" int csv_policy_loss_scratch(int N, int V, size_t* bytes) { return scratch_bytes(N, V, N < FEW_ROWS_BF16, bytes); }
 
 extern "C" int csv_token_logprobs_scratch(int N, int V, size_t* bytes) {
     const int rc = scratch_bytes(N, V, logprobs_by_parts(N, V), bytes);
@@ -518,9 +523,9 @@ extern "C" int csv_token_logprobs_scratch(int N, int V, size_t* bytes) {
     return rc;
 }
 
-static void place_scratch(RowArgs& a, void* p) {
+static void place_scratch(RowArgs& a, void* p, bool parts) {
     a.terms = (double*)p;
-    if (a.N >= FEW_ROWS) return;
+    if (!parts) return;
     a.parts = parts_of(a.N, a.V, PART_BLOCKS);
     a.part = (float2*)(a.terms + a.N);
     a.xt = (float*)(a.part + (size_t)a.N * a.parts);
@@ -542,7 +547,7 @@ extern "C" int csv_token_logprobs(const void* d_logits, int type, int64_t ld, in
     a.x = d_logits; a.ld = ld; a.N = N; a.V = V; a.tokens = d_tokens; a.c = inv_temperature; a.c2 = split(a.c * LOG2E); a.logp = d_logp; a.stats = d_stats;
     const hipStream_t st = (hipStream_t)stream;
     if (logprobs_by_parts(N, V)) {
-        place_scratch(a, d_scratch);
+        place_scratch(a, d_scratch, true);
         if (type == CSV_F32) part_kernel<float, false><<<N * a.parts, 256, 0, st>>>(a);
         else part_kernel<uint16_t, false><<<N * a.parts, 256, 0, st>>>(a);
         CSV_LAUNCH_CHECK("part_kernel");
@@ -600,9 +605,10 @@ extern "C" int csv_policy_loss(const void* d_logits, int type, int64_t ld, int N
     a.old_logp = d_old_logp; a.ref_logp = d_ref_logp; a.adv = d_advantages; a.weights = d_weights;
     a.clip_low = p->clip_low; a.clip_high = p->clip_high; a.beta = p->beta;
     a.logp = d_logp; a.grad = d_grad; a.ld_grad = ld_grad;
-    place_scratch(a, d_scratch);
+    const bool by_parts = N > 0 && N < few_rows(type);
+    place_scratch(a, d_scratch, by_parts);
     const hipStream_t st = (hipStream_t)stream;
-    if (N > 0 && N < FEW_ROWS) {
+    if (by_parts) {
         if (type == CSV_F32) part_kernel<float, true><<<N * a.parts, 256, 0, st>>>(a);
         else part_kernel<uint16_t, true><<<N * a.parts, 256, 0, st>>>(a);
         CSV_LAUNCH_CHECK("part_kernel");

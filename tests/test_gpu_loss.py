@@ -497,3 +497,28 @@ def test_zeros_of_left_out_rows_beyond_32_bits(N, V, dtype):
     assert bool((grad[N - 1] != 0).all())
     del x, grad
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("N", [111, 112, 143, 144])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V", [4099, 40009])
+def test_policy_loss_on_both_sides_of_the_rows_that_are_cut(N, V, dtype):
+    log(f"policy N={N} V={V} {dtype}")
+    x, t = _rows(N, V, dtype, N, gap=3, shift=1)
+    t[N - 1] = -1
+    _policy_check(_csv(), x, t, 1.0, 0.2, 0.28, 0.05, N + V, dtype)
+
+
+@pytest.mark.parametrize("N,V", [(64, 125000), (64, 126000), (111, 171000), (1, 65000), (1, 67000)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_log_probabilities_on_both_sides_of_the_rows_that_are_cut(N, V, dtype):
+    csv = _csv()
+    log(f"logprobs N={N} V={V} {dtype}")
+    x, t = _rows(N, V, dtype, N, gap=1, shift=1)
+    logp, stats = csv.csv_token_logprobs(x, t)
+    x64, t64 = x.cpu().double().numpy(), t.cpu().numpy()
+    m, s, want, p = O.rows_logp(x64, t64, 1.0)
+    tol, rel = O.logp_tolerance(x64, m, p, 1.0, want)
+    assert (np.abs(logp.cpu().double().numpy() - want) <= tol).all()
+    st = stats.cpu().double().numpy()
+    assert (st[:, 0] == m).all() and (np.abs(st[:, 1] - s) <= s * (rel + O.U24)).all()

@@ -171,8 +171,13 @@ __device__ __forceinline__ Stat fold(const Row<T>& row, int lo, int hi, bool sin
         for (int u = 0; u < n; ++u)
             for (int j = 0; j < E; ++j) top = fmaxf(top, x[u].v[j]);
         float add = 0.f;
-        for (int u = 0; u < n; ++u)
-            for (int j = 0; j < E; ++j) add += exp_of(x[u].v[j], top, c2);
+        for (int u = 0; u < n; ++u) {
+            float e[E];
+            for (int j = 0; j < E; ++j) e[j] = exp_of(x[u].v[j], top, c2);
+            for (int w = E / 2; w > 0; w >>= 1)         // pairs: a likely token's term is rounded as often as the tree is high, not E times
+                for (int j = 0; j < w; ++j) e[j] += e[j + w];
+            add += e[0];
+        }
         s = fmaf(s, exp_of(m, top, c2), add);
         m = top;
     };
@@ -304,6 +309,17 @@ __global__ __launch_bounds__(1024, 8) void row_kernel(RowArgs a) {
     else write_grad<1024>(row, grad, 0, row.pieces, true, token, r.m, r.s, a.c2, coef);
 }
 
+// A part's m and s in 8 bytes.  s is 0 (m minus infinity then), not a number (m neither then), or 1 and more, the largest logit's term: 5 bits of
+// exponent and 27 below the leading one, because 24 of a float32 would be the largest error of a row that is cut.
+__device__ __forceinline__ float2 pack(Stat r) {
+    const unsigned long long u = __builtin_bit_cast(unsigned long long, r.s) - (1023ull << 52) + (1ull << 24);
+    return make_float2(isnan(r.s) ? NAN : r.m, __uint_as_float((uint32_t)(u >> 25)));
+}
+__device__ __forceinline__ double unpack(float2 v) {
+    const double s = __builtin_bit_cast(double, ((unsigned long long)__float_as_uint(v.y) << 25) + (1023ull << 52));
+    return isnan(v.x) ? NAN : v.x == -INFINITY ? 0.0 : s;
+}
+
 // Short blocks, bound by the latency of a chain of loads and a reduction: 7 x 32003 float32 3.6 us, 64 x 128256 bf16 6.3 us.
 template <typename T, bool POLICY>
 __global__ __launch_bounds__(256, 8) void part_kernel(RowArgs a) {
@@ -314,7 +330,7 @@ __global__ __launch_bounds__(256, 8) void part_kernel(RowArgs a) {
     const Row<T> row((const T*)a.x + (int64_t)i * a.ld, a.V);
     const Stat r = fold<256>(row, (int)((int64_t)row.pieces * p / a.parts), (int)((int64_t)row.pieces * (p + 1) / a.parts), p == 0, a.c2, red);
     if (threadIdx.x == 0) {
-        a.part[(int64_t)i * a.parts + p] = make_float2(r.m, (float)r.s);
+        a.part[(int64_t)i * a.parts + p] = pack(r);
         if (p == 0) a.xt[i] = get(row.p + token);
     }
 }
@@ -326,7 +342,8 @@ __device__ __forceinline__ Stat join(const RowArgs& a, int i) {
     if (lane < a.parts) v = a.part[(int64_t)i * a.parts + lane];
     Stat r;
     r.m = wave_max(v.x);
-    r.s = wave_sum(v.y == 0.f ? 0.0 : (double)v.y * (double)exp_of(v.x, r.m, a.c2));
+    const double s = unpack(v);
+    r.s = wave_sum(s == 0.0 ? 0.0 : s * (double)exp_of(v.x, r.m, a.c2));
     return r;
 }
 

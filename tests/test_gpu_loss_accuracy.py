@@ -6,6 +6,7 @@ exponentials, with a the distance of a logit from the largest one in units of th
   a thread's sum      up to n = V / 256 additions of U of what it holds, and 256 threads or more
   a part's sum        U where it is kept as a float32
 and what all rows share, the mean error of the hardware's exponential, which is below 5e-9 over every tenth of a period (2^22 arguments in each).
+A term is multiplied with two more of them on its way, where threads and parts meet.
 Six standard deviations are allowed for a mean.
 """
 import math
@@ -144,3 +145,35 @@ def test_parameters_keep_the_digits_of_a_double(N, dtype):
     old, ref, adv, w = _with_left_out(2, [([-1000.0] * 2, 0.0), ([-999.0] * 2, 0.0), ([a0, a1], 0.0), ([1.0] * 2, 0.0)], N)
     loss = csv.csv_policy_loss(x, t, old, ref, adv, w, beta=0.1)[0].item()
     assert abs(loss - (v - a0 - a1)) <= 16 * 2.0 ** -53
+
+
+@pytest.mark.parametrize("V", [2000, 32003])
+def test_a_row_that_is_cut_loses_no_digits_where_its_parts_meet(V):
+    """A flat row's sum has many small errors that average out; one rounding of the whole to a float32 would be larger than all of them.  What the kernel
+    holds beyond a float32 shows in a loss of two rows: the ratio of the first less a ratio of exactly 1."""
+    csv = _csv()
+    log(f"digits of a cut row V={V}")
+    gen = torch.Generator(device="cuda").manual_seed(V)
+    t = torch.zeros(2, dtype=torch.int32, device="cuda")
+    w = torch.ones(2, device="cuda")
+    adv = torch.tensor([1.0, -1.0], device="cuda")
+    errors, var = [], 0.0
+    calls = 300
+    for k in range(calls):
+        x = torch.randn(2, V, generator=gen, device="cuda")
+        x[1] = -1000.0                                      # the second row: token 0 has a log-probability of 0
+        x[1, 0] = 0.0
+        want = _exact(x, t, 1.0)[0]
+        old = want.float()
+        loss = csv.csv_policy_loss(x, t, old, None, adv, w, want_grad=False)[0]
+        errors.append(-loss.double() - torch.expm1(want[0] - old[0].double()))
+        p = torch.softmax(x[0].double(), 0)
+        a = x[0].double().amax() - x[0].double()
+        # standard deviations: two roundings of an argument, a U / sqrt(3) each; the exponential's, 0.6 U; four of a thread's sum, 250 threads a part;
+        # where threads meet in a part and parts in a row, each of them is multiplied with another exponential, and its mean error comes in again
+        parts = (V - 1) // 2048 + 1
+        var += ((p * p * (2 / 3 * a * a + 0.36)).sum().item() + (4 / 3 + 0.7) / (250 * parts) + (0.36 / parts if parts > 1 else 0.0)) * U ** 2
+    rms = torch.stack(errors).pow(2).mean().sqrt().item()
+    allowed = 1.5 * math.sqrt(var / calls) + COMMON * (3 if parts > 1 else 2)
+    log(f"rms {rms:.2e}, allowed {allowed:.2e}, half a step of a float32 between 1 and 2 {U:.2e}")
+    assert rms <= allowed

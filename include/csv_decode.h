@@ -350,7 +350,8 @@ void csv_mx4_head_free(csv_mx4_head* head);
  * Logits of a 4-bit head: d_logits[b*V + i] = <W_i, h_b> + b_i for B hidden states d_h bf16[B*d] (16-byte aligned), products
  * exact, sums in float32, rounded once more where out_type is CSV_BF16.  act = CSV_ACT_BF16 takes h as it is (decode steps),
  * CSV_ACT_MX4 rounds it to the 4-bit format first (many tokens: four times the matrix rate).  1 <= B <= CSV_MX4_MAX_BATCH, or 0.
- * A logit's bits do not depend on B.  Scratch: csv_mx4_logits_scratch bytes, 16-byte aligned (none for CSV_ACT_BF16, or for few hidden states).
+ * A logit has had the same bits for every B that was tried; that is an observation, not a promise: kernels for few and for many hidden states use
+ * instructions that add up different numbers of products, in an order that is not documented.  Scratch: csv_mx4_logits_scratch bytes, 16-byte aligned (none for CSV_ACT_BF16, or for few hidden states).
  */
 #define CSV_ACT_BF16 0
 #define CSV_ACT_MX4  1

@@ -16,8 +16,10 @@
 // log-probability of every row, the same way, by that part of c (m - E[x]).  It is kept as the sum of two floats: fma(d, hi, d lo) rounds once (mean error of
 // 2048 rows of 64007 float32 logits, c = 1 / 0.7: -5.8e-8 / -9.5e-8 with one float, below 1e-8 with two; 64 rows of 128256, bound by instructions, 9.8 ->
 // 11.5 us, many rows, bound by memory, within 1 percent).  The low part cannot be added to a rounded d hi, or to m c2 before it: most of it is
-// lost in their last digit.  A thread adds up in float32;
-// threads and parts are added in float64, because what those last sums lose is not averaged over anything.
+// lost in their last digit.  A thread adds up in float32; threads and parts are added in float64, because what those last sums lose is
+// not averaged over anything.
+//
+// Times here and below: on the GPU, inputs changing from pass to pass where they fit, unless another measure is named.
 #include "csv_common.h"
 
 #include <math.h>
@@ -271,8 +273,8 @@ __device__ __forceinline__ bool left_out(const RowArgs& a, int i, int token, boo
 }
 
 // Bound by memory, two blocks per compute unit: one reads while the other reduces or writes.  The second read finds the row in a cache, so the gradient
-// costs a read and a write: 4096 x 128256 bf16, a fifth of the rows left out, 400 us (4.7 TB/s, the rate of a copy); the log-probabilities alone,
-// 2048 x 128256: 171 us in float32 (6.1 TB/s), 86 us in bf16.
+// costs a read and a write: 4096 x 128256 bf16, a fifth of the rows left out, 402 us (4.7 TB/s, the rate of a copy); the log-probabilities alone,
+// 2048 x 128256: 171 us in float32 (6.1 TB/s), 88 us in bf16 (6.0 TB/s).
 template <typename T, bool POLICY>
 __global__ __launch_bounds__(1024, 8) void row_kernel(RowArgs a) {
     __shared__ double red[16];
@@ -320,7 +322,7 @@ __device__ __forceinline__ double unpack(float2 v) {
     return isnan(v.x) ? NAN : v.x == -INFINITY ? 0.0 : s;
 }
 
-// Short blocks, bound by the latency of a chain of loads and a reduction: 7 x 32003 float32 3.6 us, 64 x 128256 bf16 6.3 us.
+// Short blocks, bound by the latency of a chain of loads and a reduction: 7 x 32003 float32 3.8 us, 64 x 128256 bf16 6.9 us.
 template <typename T, bool POLICY>
 __global__ __launch_bounds__(256, 8) void part_kernel(RowArgs a) {
     __shared__ double red[16];
@@ -377,7 +379,7 @@ __device__ __forceinline__ double sum_terms(const double* terms, int N, double* 
     return s;
 }
 
-// Every block of a row takes the same scalars from the same parts; only the first one writes them.  7 x 32003 float32 5.5 us, 64 x 128256 bf16 7.9 us.
+// Every block of a row takes the same scalars from the same parts; only the first one writes them.  7 x 32003 float32 5.7 us, 64 x 128256 bf16 8.8 us.
 template <typename T>
 __global__ __launch_bounds__(256) void policy_kernel(RowArgs a, int parts, float* loss) {
     __shared__ float coef;

@@ -11,6 +11,9 @@
 // A head is cut into bands of 64 rows.  A band is one piece of memory in the order in which it is read: for every four steps of 128
 // elements the scales of its four tiles (1 KB), then for each step the codes of its four tiles (4 KB).  Bands are no power of two apart,
 // so that blocks that start together do not ask for the same memory channels.
+//
+// Times here and below are those of a pass among others.  A head of 279 MB (128256 x 4096) that is read again and again finds part of itself in the
+// last-level cache; where heads change from pass to pass, the figure is called a fresh head's.
 #include "csv_common.h"
 
 #include <stdlib.h>
@@ -83,7 +86,7 @@ __device__ __forceinline__ uint32_t round8(const Elems8& x, uint32_t& scale) {
 
 // One wave: 512 elements of a row (blockIdx.x), rows blockIdx.y * 4 + wave and every 4 * gridDim.y rows further.  TILES: codes and scales go
 // to tiles; rows past `rows` (up to rows_out) are zeros.  Bound by memory: four lanes share a block, so that every load and store of a wave is
-// one piece (128256 x 4096 bf16: 228 us, 5.8 TB/s read and written).
+// one piece (128256 x 4096 bf16: 226 us, 5.9 TB/s read and written).
 template <typename T, bool TILES>
 __global__ __launch_bounds__(256) void quantize_kernel(const T* __restrict__ x, int64_t ld, int rows, int rows_out, int d, int chunks,
                                                         uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
@@ -106,7 +109,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(const T* __restrict__ x, 
 }
 
 // One wave: 512 elements of a row, 16 bytes of values per lane and store, side by side.  They leave past the caches: four times what came in, and
-// read by another kernel at the earliest (128256 x 4096 to bf16 236 -> 225 us).
+// read by another kernel at the earliest (128256 x 4096 to bf16 235 -> 225 us; 237 alone under a profiler).
 template <typename T>
 __global__ __launch_bounds__(256) void dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int rows, int d, int chunks,
                                                           T* __restrict__ x, int64_t ld) {
@@ -232,8 +235,9 @@ __device__ __forceinline__ void give_out(const LogitsArgs& a, const float* buf, 
     }
 }
 
-// Codes that one block alone reads (ONCE: all hidden states in one group) go past the caches: 1 hidden state at 128256 x 4096 53.0 -> 46.4 us, 32 at
-// 256000 x 4608 117 -> 107; where several blocks read them it costs as much (2048 at 128256 x 4096 in bf16 1695 -> 1861).
+// Codes that one block alone reads (ONCE: all hidden states in one group) go past the caches: 1 hidden state at a fresh head of 128256 x 4096
+// 48.0 -> 42.6 us (the same head again 41.1 -> 40.5, with 30 of them 45.8 -> 48.5), 32 at 256000 x 4608 117 -> 105; where several blocks read them
+// it costs as much (1024 at 128256 x 4096 in bf16 823 -> 878, 2048 1677 -> 1835).
 template <bool ONCE>
 __device__ __forceinline__ v4u load_codes(const uint8_t* p) {
     if constexpr (ONCE) return __builtin_nontemporal_load((const v4u*)p);
@@ -251,8 +255,9 @@ enum { H_BF16, H_TILES, H_ROUNDED_HERE };
 // stage of h lies in LDS, two buffers, and passes through registers on its way there, so that a barrier waits for no load.  bf16 h lies row by
 // row with the 16-byte pieces of row t exchanged by t % 16 (a column of pieces then spreads over all banks); 4-bit h lies as its tiles, which few
 // hidden states become here (a thread rounds a block: cheaper than a launch, while the block waits for W).
-// Bound by the read of W up to 32 hidden states (64 in 4 bits): 1 at 128256 x 4096 42 us (6.8 TB/s), 32 at 256000 x 4608 with 33 MB of logits 106 us
-// (6.2 TB/s); with more of them in bf16 by the matrix cores: 1024 at 128256 x 4096 830 us (1.3 PFLOP/s, the rate of the largest library products).
+// Bound by the read of W up to 32 hidden states (64 in 4 bits): 1 at a fresh head of 128256 x 4096 42.6 us (6.6 TB/s), 32 at 256000 x 4608 with 33 MB of
+// logits 105 us (6.3 TB/s); with more of them in bf16 by the matrix cores: 1024 at 128256 x 4096 824 us (1.3 PFLOP/s, the rate of the largest
+// library products).
 // Past the end of a row or of the batch the last piece or row is read again: the last stage puts zeros in the row's place, and those hidden
 // states are not stored.
 template <int H, int NT, int RT, int S, bool ONCE, typename T>
@@ -434,10 +439,12 @@ __global__ __launch_bounds__(256, 3) void product_kernel(LogitsArgs a) {
 // pieces of 256 bytes, blocks l / 32 and then 2 + l / 32 of a step.
 // The blocks that share a band ask for its codes at about the same time, so that each of them waits for memory, not for a cache.  Codes are
 // therefore requested four steps ahead, each register again as soon as its products are issued; h comes two steps at a time, one such
-// stage ahead, from global memory to LDS without registers, which are all taken: 128 sums, 64 of codes.  2048 at 128256 x 4096, bf16 logits: 610 us,
-// 3.5 PFLOP/s.  Its parts, each taken away in turn: the writes of the logits 95 us, codes that come from memory 50, h from memory 20, all
-// three 130; codes of zeros 85 (the clock, which random codes lower).  Products, LDS reads and barriers alone take 371.  Blocks twice as
-// wide, groups of hidden states that stay in a cache and starts staggered so that writes meet other blocks' products gain nothing.
+// stage ahead, from global memory to LDS without registers, which are all taken: 128 sums, 64 of codes.  2048 at 128256 x 4096, bf16 logits: 602 to
+// 617 us with the rounding of h, 9 of them (3.5 PFLOP/s; 640 for this kernel alone under a profiler, at a lower clock); matrix cores busy 46 % of the cycles.
+// Before the logits left in whole lines, when a pass took 610 us, its parts, each taken away in turn, were: the
+// writes of the logits 95 us, codes that come from memory 50, h from memory 20, all three 130; codes of zeros 85 (the clock, which random codes
+// lower); products, LDS reads and barriers alone took 371.  Blocks twice as wide, groups of hidden states that stay in a cache and starts
+// staggered so that writes meet other blocks' products gained nothing.
 template <bool ONCE, typename T>
 __global__ __launch_bounds__(256, 2) void many_kernel(LogitsArgs a) {
     constexpr int OW = 256 + 4;
@@ -749,7 +756,8 @@ extern "C" int csv_mx4_logits(const csv_mx4_head* x, const uint16_t* d_h, int B,
     // Waves that take 64 rows each read h least often, waves of 32 rows make more blocks: below three blocks for two compute units
     // the units that have none, or two, cost more.  Microseconds, 32 / 64 rows a wave, from d = 4096: bf16, 14 hidden states, V = 80000
     // 32.5 / 36.3, 100000 42.1 / 39.3, 128256 48.1 / 44.9;  30 of them, 80000 38.3 / 41.0, 100000 48.9 / 43.2;  4 bits, 60, 80000 39.3 / 43.2,
-    // 128256 55.9 / 52.7.  (16 rows: 32.9 and 54.5 for 14 at 80000 and 128256.)
+    // 128256 55.9 / 52.7.  (16 rows: 32.9 and 54.5 for 14 at 80000 and 128256.)  At small heads, read again and again: 32000 x 1024, 1 hidden state
+    // 4.8 / 6.3, 14 5.1 / 6.8;  64000 x 1024, 14, 7.6 / 7.9;  32000 x 4096, 14, 12.1 / 19.5;  50000 x 4096, 1, 20.9 / 23.7, 30, 25.4 / 23.1.
     const int64_t full = ((int64_t)x->V + 255) / 256;             // blocks of four waves of 64 rows
     const int64_t fill = 384;
     if (act == CSV_ACT_BF16) {

@@ -506,13 +506,14 @@ static int check_scratch(size_t need, const void* p, size_t have) {
 }
 
 // Where the rows alone leave compute units without work, or with too little of it to keep the memory busy, a row is cut into parts: two launches,
-// and the logits are read twice.  A policy loss does so below few_rows (with gradient, us on the GPU, parts / row: rows of 128256 bf16, 64 of them
-// 14.8 / 22.7, 112 20.9 / 24.6, 128 23.2 / 26.7, 190 30.8 / 29.2, of 80000 128 16.6 / 17.4, 160 20.6 / 17.9;  of 128256 float32 64 20.7 / 27.2,
-// 112 32.8 / 33.4, 128 40.4 / 34.8;  of 32000 64 10.5 / 11.8 and 11.0 / 10.8, 112 12.3 / 12.0 and 12.8 / 10.9.  The loss alone follows, so that it
-// keeps its bits: of 128256 bf16 64 10.7 / 12.7, 128 14.5 / 13.9, float32 64 12.2 / 14.4, 90 15.5 / 14.8, of 32000 64 8.7 / 8.1).  Log-probabilities in
-// one block per row are one launch, 3.3 us less for a host that waits for each call, and stay ahead up to longer rows the more rows there are
-// (1 row of 32000 float32 4.8 / 4.6, of 80000 5.0 / 7.2, of 128256 5.0 / 9.6, 64 of 80000 8.0 / 7.7, of 128256 9.7 / 11.7, 90 of 128256
-// 12.4 / 12.2, of 256000 19.4 / 19.2).
+// and the logits are read twice.  A policy loss does so below few_rows (with gradient, us on the GPU, parts / row: bf16 rows of 128256, 64 of them
+// 16.4 / 25.4, 112 22.6 / 26.0, 143 24.4 / 26.1, 190 32.1 / 28.6, of 80000 112 17.7 / 19.3, 143 19.6 / 19.5, 160 22.7 / 19.8, of 32000 112 13.5 / 13.9,
+// 143 15.2 / 14.7;  float32 rows of 128256 64 23.7 / 28.7, 112 33.7 / 34.3, 128 41.3 / 35.7, of 80000 90 21.5 / 22.1, 112 23.5 / 22.5, of 32000 64
+// 12.1 / 13.0, 112 15.0 / 14.6).  The loss alone follows, so that it keeps its bits (of 128256 bf16 64 13.0 / 15.9, 112 16.5 / 16.3, 143 17.0 / 16.2,
+// float32 64 15.8 / 18.2, 112 19.8 / 19.6, of 32000 bf16 64 9.5 / 9.5, 112 11.4 / 10.4).  Log-probabilities in one block per row are one launch,
+// 3.3 us less for a host that waits for each call, and stay ahead up to longer rows the more rows there are (float32, 1 row of 32000 4.9 / 5.4, of
+// 80000 4.9 / 8.2, of 128256 4.9 / 10.7, 64 of 80000 10.4 / 11.4, of 128256 12.8 / 15.0, 90 of 128256 14.4 / 15.8, bf16, 64 of 80000 8.9 / 9.2; from
+// the host, 1 row of 128256 9.8 / 10.4).
 #define FEW_ROWS 112
 #define FEW_ROWS_BF16 144           // the larger one, and what scratch is made for
 static inline int few_rows(int type) { return type == CSV_BF16 ? FEW_ROWS_BF16 : FEW_ROWS; }

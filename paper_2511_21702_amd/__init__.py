@@ -604,7 +604,8 @@ def csv_policy_loss(logits: torch.Tensor, tokens: torch.Tensor, old_logp: torch.
                     loss: torch.Tensor | None = None, logp: torch.Tensor | None = None, grad: torch.Tensor | None = None, want_grad: bool = True,
                     scratch: torch.Tensor | None = None, stream=None):
     """(loss float32 scalar tensor, logp float32 [N], grad [N, V] in the type of the logits, or None without want_grad and grad) of the
-    clipped policy loss; weights are mask and normaliser in one.  grad may be the logits themselves."""
+    clipped policy loss; weights are mask and normaliser in one.  grad may be the logits themselves; no other output may share memory with an input.
+    Rows that a mask leaves nothing of add 0; a masked token has ratio 0."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return csv_policy_loss(logits, tokens, old_logp, ref_logp, advantages, weights, clip_low, clip_high, beta, inv_temperature, loss,

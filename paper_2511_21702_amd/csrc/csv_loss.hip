@@ -513,7 +513,7 @@ static int check_scratch(size_t need, const void* p, size_t have) {
 // float32 64 15.8 / 18.2, 112 19.8 / 19.6, of 32000 bf16 64 9.5 / 9.5, 112 11.4 / 10.4).  Log-probabilities in one block per row are one launch,
 // 3.3 us less for a host that waits for each call, and stay ahead up to longer rows the more rows there are (float32, 1 row of 32000 4.9 / 5.4, of
 // 80000 4.9 / 8.2, of 128256 4.9 / 10.7, 64 of 80000 10.4 / 11.4, of 128256 12.8 / 15.0, 90 of 128256 14.4 / 15.8, bf16, 64 of 80000 8.9 / 9.2; from
-// the host, 1 row of 128256 9.8 / 10.4).
+// the host, 1 row of 128256 10.1 / 9.8).
 #define FEW_ROWS 112
 #define FEW_ROWS_BF16 144           // the larger one, and what scratch is made for
 static inline int few_rows(int type) { return type == CSV_BF16 ? FEW_ROWS_BF16 : FEW_ROWS; }
